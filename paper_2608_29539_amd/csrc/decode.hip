@@ -27,6 +27,7 @@
 // The cache is read once per branch (HBM-bound); the arithmetic is fp32
 // (bf16 dot products accumulate in fp32 with v_dot2), so no MFMA is needed.
 #include "logo_internal.h"
+#include "decode_common.h"
 
 namespace logo {
 namespace {
@@ -66,45 +67,6 @@ __device__ __forceinline__ float row16_sum(float x) {
     return x;
 }
 
-// The token's routing decision z_b = gate[b] > thr (fp32, strict: a NaN
-// gate or threshold selects nothing), taken identically by every workgroup
-// that needs it.
-__device__ __forceinline__ float decode_threshold(const DecodeArgs &a) {
-    return a.sel_mode == 2 ? a.thr_dev[0] : a.thr_host;
-}
-
-// The compacted list of selected sequences (ascending) and the count, each
-// where it is asked for: one workgroup, ballot + mbcnt ranks and a carry over
-// chunks of kDecThreads sequences.
-__device__ void build_active_list(const DecodeArgs &a) {
-    __shared__ int s_cnt[kDecThreads / 64];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const float thr = decode_threshold(a);
-    int carry = 0;
-    for (int c0 = 0; c0 < a.num_seqs; c0 += kDecThreads) {
-        const int b = c0 + tid;
-        const bool z = b < a.num_seqs && a.gate[b] > thr;
-        const uint64_t m = __ballot(z);
-        const int below = (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32),
-                                                        __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0));
-        if (lane == 0)
-            s_cnt[wave] = (int)__popcll(m);
-        __syncthreads();
-        int before = carry, total = 0;
-        for (int i = 0; i < kDecThreads / 64; i++) {
-            if (i < wave)
-                before += s_cnt[i];
-            total += s_cnt[i];
-        }
-        if (z && a.act)
-            a.act[before + below] = b;
-        carry += total;
-        __syncthreads();                         // s_cnt is rewritten by the next chunk
-    }
-    if (tid == 0 && a.n_act)
-        a.n_act[0] = carry;
-}
-
 // (m, l, acc) of stream b merged into stream a (exp2 domain).
 __device__ __forceinline__ void merge_into(float &ma, float &la, float &mb, float &lb, float *aa,
                                            const float *ab, int n) {
@@ -130,7 +92,7 @@ __global__ __launch_bounds__(kDecThreads) void decode_attn_kernel(const DecodeAr
     const int per_row = a.hkv * a.nhg;
     int item = blockIdx.x;
     if (item == a.n_local_items + a.n_global_items) {
-        build_active_list(a);
+        build_active_list<kDecThreads>(a);
         return;
     }
     const bool global = item >= a.n_local_items;
