@@ -79,7 +79,10 @@ typedef enum {
     LOGO_ENTRY_BWD = 8,
     LOGO_ENTRY_DENSE_BWD = 9,
     LOGO_ENTRY_GLOBAL_BWD = 10,
-    LOGO_ENTRY_FWD_QPHI = 11
+    LOGO_ENTRY_FWD_QPHI = 11,
+    LOGO_ENTRY_CACHE_SCORE = 12,
+    LOGO_ENTRY_DECODE_SCORE = 13,
+    LOGO_ENTRY_CACHE_EVICT = 14
 } logo_entry;
 
 /* Problem description (a host struct; only cu_seqlens is a device pointer). */
@@ -450,6 +453,144 @@ logo_status logo_decode_noalloc(const logo_problem *p, const logo_bf16 *q, const
                                 float threshold, const float *thr_dev, const float *gain_local,
                                 const float *gain_global, float eps, logo_bf16 *out,
                                 int32_t *active, int32_t *n_active, logo_stream stream);
+
+/* Prefixes that groups of sequences share (a host struct; cu_prefix and
+ * cu_group are device pointers).  Prefix r holds rows cu_prefix[r] ..
+ * cu_prefix[r+1]-1 of the prefix tensors and belongs to sequences cu_group[r]
+ * .. cu_group[r+1]-1; a prefix may be empty, and so may a group. */
+typedef struct {
+    int32_t num_prefixes;           /* R >= 1                                            */
+    int32_t total_tokens;           /* rows of the prefix tensors = cu_prefix[R] >= 0    */
+    int32_t max_prefix;             /* >= every prefix's length                          */
+    int32_t max_group;              /* >= every group's sequences; 1 .. num_seqs         */
+    const int32_t *cu_prefix;       /* device [R+1]: 0 = cu[0] <= ... = total_tokens     */
+    const int32_t *cu_group;        /* device [R+1]: 0 = cu[0] <= ... = num_seqs         */
+    const int32_t *cu_prefix_host;  /* optional host copies (NULL allowed), checked      */
+    const int32_t *cu_group_host;   /* against the sizes above                           */
+} logo_prefix;
+
+/*
+ * logo_decode_prefix -- logo_decode for sequences that share prefixes: the
+ * cache of sequence b of prefix r is [prefix r ; its own rows], P_r + S_b
+ * keys, and the step is logo_decode's on that cache (Sec. 3.3 and App. B,
+ * Autoregressive Decoding): the new token's query attends to the last
+ * min(P_r + S_b, w) keys, which may reach into the prefix, a selected token's
+ * also to all of them.  A prefix's rows are read once for its group.
+ *   p          cu_seqlens = the sequences' own rows: S_b rows of k / v, the
+ *              last of which is the new token's own key and value (appended by
+ *              the caller).  S_b = 0 is allowed where P_r > 0.  With all host
+ *              copies given, P_r + S_b = 0 is rejected (LOGO_ERR_SHAPE);
+ *              without them such a sequence outputs zeros.
+ *   k_pre, v_pre   device [prefix->total_tokens][Hkv][d] bf16.
+ *   q, k, v, gate, mode, threshold, thr_dev, gain_local, gain_global, eps, out,
+ *   active, n_active   as for logo_decode.
+ *   q_g, k_pre_g, v_pre_g, k_g, v_g   the global branch's tensors: q_g alone,
+ *              the four caches together, or both (NULL = the local ones);
+ *              LOGO_ERR_ARG for some of the caches without the others.
+ *   All bf16 tensors 16-byte aligned (LOGO_ERR_ARG).
+ *   The values of a prefix must be finite: one that is not may reach, through
+ *   a product with a zero weight, sequences of its group whose window leaves
+ *   it out.
+ *   Numerics: P is rounded to bf16 for the product with V (as in
+ *   logo_attn_fwd), everything else is fp32; the result does not depend on
+ *   the order in which workgroups run.
+ *   ws >= logo_decode_prefix_workspace_bytes(p, prefix) bytes, 256-byte
+ *   aligned (partial results of the key chunks).
+ */
+logo_status logo_decode_prefix(const logo_problem *p, const logo_prefix *prefix,
+                               const logo_bf16 *q, const logo_bf16 *k_pre, const logo_bf16 *v_pre,
+                               const logo_bf16 *k, const logo_bf16 *v, const logo_bf16 *q_g,
+                               const logo_bf16 *k_pre_g, const logo_bf16 *v_pre_g,
+                               const logo_bf16 *k_g, const logo_bf16 *v_g, const float *gate,
+                               logo_sel_mode mode, float threshold, const float *thr_dev,
+                               const float *gain_local, const float *gain_global, float eps,
+                               logo_bf16 *out, int32_t *active, int32_t *n_active, void *ws,
+                               size_t ws_bytes, logo_stream stream);
+
+/* Workspace size of logo_decode_prefix; 0 for an invalid problem or prefix. */
+size_t logo_decode_prefix_workspace_bytes(const logo_problem *p, const logo_prefix *prefix);
+
+/*
+ * logo_cache_score -- the attention weight that every key of the global
+ * branch received from the selected rows (Eq. query-sparse-global), added to
+ * what earlier rows left:
+ *   score[h][j] = score_in[h][j] + sum_i sum_{g < G} 2^(c q_{i,hG+g} . k_{j,h} - lse_{i,hG+g})
+ * over the selected rows i at or after key j of its sequence, G = Hq / Hkv, c =
+ * softmax_scale * log2(e).  The heads of a KV head add to the same key, as they
+ * read it together.
+ *   q [N][Hq][d], k [N][Hkv][d] bf16, 16-byte aligned (LOGO_ERR_ARG): the
+ *              global branch's.
+ *   sel_idx, cu_sel, sel_capacity   the rows, as for logo_global_attn_sparse_q
+ *              (only the first min(cu_sel[B], sel_capacity) count); both NULL:
+ *              every token is a row (sel_capacity is ignored, N in its place).
+ *   lse        device [Hq][sel_capacity] fp32: base-2 log-sum-exp of the
+ *              rows' scaled scores, as logo_global_attn_sparse_q_fwd_train,
+ *              logo_attn_fwd_train (lse_global) or, for every token,
+ *              logo_dense_causal_attn_fwd_train keep it.  NULL: computed here.
+ *   score_in   device [Hkv][N] fp32, or NULL for zeros; may be score.
+ *   score      device [Hkv][N] fp32, every entry written.
+ *   ws         only with lse NULL: >= logo_workspace_bytes(p,
+ *              LOGO_ENTRY_CACHE_SCORE, sel_capacity) bytes, 256-byte aligned.
+ * fp32 sums in a fixed order: the same call gives the same bits.
+ */
+logo_status logo_cache_score(const logo_problem *p, const logo_bf16 *q, const logo_bf16 *k,
+                             const int32_t *sel_idx, const int32_t *cu_sel, int32_t sel_capacity,
+                             const float *lse, const float *score_in, float *score, void *ws,
+                             size_t ws_bytes, logo_stream stream);
+
+/*
+ * logo_decode_score -- the same for one decoding step: the weights that each
+ * selected sequence's new token (gate above the threshold, as in logo_decode)
+ * gives its L_b cached keys; the keys of the other sequences keep score_in.
+ *   p, q [B][Hq][d], k [N][Hkv][d], gate, mode, threshold, thr_dev   as for
+ *              logo_decode (of the global branch: q_g, k_g); q and k 16-byte
+ *              aligned (LOGO_ERR_ARG).
+ *   score_in, score   as for logo_cache_score.
+ *   ws >= logo_workspace_bytes(p, LOGO_ENTRY_DECODE_SCORE, 0) bytes, 256-byte
+ *   aligned (the scores: 4 Hq N bytes and the chunks' sums).
+ */
+logo_status logo_decode_score(const logo_problem *p, const logo_bf16 *q, const logo_bf16 *k,
+                              const float *gate, logo_sel_mode mode, float threshold,
+                              const float *thr_dev, const float *score_in, float *score, void *ws,
+                              size_t ws_bytes, logo_stream stream);
+
+/*
+ * logo_cache_evict -- caches cut down to `budget` rows per sequence and KV
+ * head.  Of a sequence's L rows n = min(L, budget) stay: its last
+ * min(recent, n), and of the others those with the largest scores (a NaN is the
+ * lowest, -0 equals +0, ties go to the lowest index), in ascending order.  The
+ * results are packed caches with cu_seqlens cu_keep, which logo_decode,
+ * logo_decode_prefix and logo_decode_score read; with recent >= w - 1 the local
+ * branch of the next step sees what it would have seen.  KV heads keep rows of
+ * their own, so row i of the result holds other positions for each head.
+ *   p          cu_seqlens = the caches; window and num_q_heads are not used.
+ *   score      device [Hkv][N] fp32.
+ *   budget >= 1, recent >= 0 (LOGO_ERR_ARG).
+ *   k, v       device [N][Hkv][d] bf16, or both NULL (then only the choice is
+ *              made); k_g, v_g likewise, cut by the same choice.  k_out, v_out,
+ *              k_g_out, v_g_out [capacity][Hkv][d]: given exactly where their
+ *              inputs are (LOGO_ERR_ARG).  16-byte aligned (LOGO_ERR_ARG).
+ *   score_out  device [Hkv][capacity] fp32: the kept rows' scores.
+ *   keep_idx   device [Hkv][capacity] int32: the kept rows, as rows of the
+ *              input caches.
+ *   cu_keep    device [B+1] int32.
+ *   capacity   >= logo_cache_keep_capacity(p, budget) (LOGO_ERR_SHAPE): the
+ *              rows of the outputs and the stride of score_out and keep_idx.
+ *   Rows of the outputs at or past cu_keep[B] are left as they were.  No output
+ *   may overlap an input.
+ *   ws >= logo_workspace_bytes(p, LOGO_ENTRY_CACHE_EVICT, 0) bytes, 256-byte
+ *   aligned.
+ */
+logo_status logo_cache_evict(const logo_problem *p, const float *score, int32_t budget,
+                             int32_t recent, const logo_bf16 *k, const logo_bf16 *v,
+                             const logo_bf16 *k_g, const logo_bf16 *v_g, logo_bf16 *k_out,
+                             logo_bf16 *v_out, logo_bf16 *k_g_out, logo_bf16 *v_g_out,
+                             float *score_out, int32_t *keep_idx, int32_t *cu_keep,
+                             int32_t capacity, void *ws, size_t ws_bytes, logo_stream stream);
+
+/* Rows that logo_cache_evict can keep: sum_b min(L_b, budget) from
+ * cu_seqlens_host, or min(N, B budget) when that is NULL.  -1 on bad input. */
+int64_t logo_cache_keep_capacity(const logo_problem *p, int32_t budget);
 
 /*
  * logo_gate_proj -- the gate of Eq. gate-routing (Sec. 3.2):

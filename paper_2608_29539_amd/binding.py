@@ -30,6 +30,9 @@ LOGO_ENTRY_BWD = 8
 LOGO_ENTRY_DENSE_BWD = 9
 LOGO_ENTRY_GLOBAL_BWD = 10
 LOGO_ENTRY_FWD_QPHI = 11
+LOGO_ENTRY_CACHE_SCORE = 12
+LOGO_ENTRY_DECODE_SCORE = 13
+LOGO_ENTRY_CACHE_EVICT = 14
 LOGO_PHI_LP = 0
 LOGO_PHI_SO = 1
 
@@ -42,7 +45,8 @@ EXPORTS = (
     "logo_attn_fwd_train", "logo_attn_bwd", "logo_dense_causal_attn_fwd_train",
     "logo_dense_causal_attn_bwd", "logo_global_attn_sparse_q_fwd_train",
     "logo_global_attn_sparse_q_bwd", "logo_decode_noalloc", "logo_attn_fwd_qphi",
-    "logo_attn_fwd_launches",
+    "logo_attn_fwd_launches", "logo_decode_prefix", "logo_decode_prefix_workspace_bytes",
+    "logo_cache_score", "logo_decode_score", "logo_cache_evict", "logo_cache_keep_capacity",
 )
 
 _lib = None
@@ -69,6 +73,19 @@ class _Problem(ctypes.Structure):
     ]
 
 
+class _Prefix(ctypes.Structure):
+    _fields_ = [
+        ("num_prefixes", ctypes.c_int32),
+        ("total_tokens", ctypes.c_int32),
+        ("max_prefix", ctypes.c_int32),
+        ("max_group", ctypes.c_int32),
+        ("cu_prefix", ctypes.c_void_p),
+        ("cu_group", ctypes.c_void_p),
+        ("cu_prefix_host", ctypes.c_void_p),
+        ("cu_group_host", ctypes.c_void_p),
+    ]
+
+
 def library_path() -> str:
     return _LIB_PATH
 
@@ -85,7 +102,7 @@ def library():
     lib = ctypes.CDLL(_LIB_PATH)
     P, i32, i64, f32, f64, sz = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64,
                                  ctypes.c_float, ctypes.c_double, ctypes.c_size_t)
-    PP = ctypes.POINTER(_Problem)
+    PP, PX = ctypes.POINTER(_Problem), ctypes.POINTER(_Prefix)
     sigs = {
         "logo_select": [PP, P, i32, f32, f64, P, i32, P, P, P, P, sz, P],
         "logo_local_attn": [PP, P, P, P, P, P],
@@ -111,6 +128,11 @@ def library():
         "logo_dense_causal_attn_bwd": [PP, P, P, P, P, P, P, P, P, P, P, sz, P],
         "logo_attn_bwd": [PP, P, P, P, P, P, P, P, P, P, f32, P, i32, P, P, P, P, P, P, P, P, P,
                           P, P, P, P, P, P, P, P, sz, P],
+        "logo_decode_prefix": [PP, PX, P, P, P, P, P, P, P, P, P, P, P, i32, f32, P, P, P, f32, P,
+                               P, P, P, sz, P],
+        "logo_cache_score": [PP, P, P, P, P, i32, P, P, P, P, sz, P],
+        "logo_decode_score": [PP, P, P, P, i32, f32, P, P, P, P, sz, P],
+        "logo_cache_evict": [PP, P, i32, i32, P, P, P, P, P, P, P, P, P, P, P, i32, P, sz, P],
     }
     for name, args in sigs.items():
         fn = getattr(lib, name)
@@ -122,6 +144,10 @@ def library():
     lib.logo_ratio_capacity.restype = i64
     lib.logo_attn_fwd_launches.argtypes = [PP]
     lib.logo_attn_fwd_launches.restype = ctypes.c_int
+    lib.logo_decode_prefix_workspace_bytes.argtypes = [PP, PX]
+    lib.logo_decode_prefix_workspace_bytes.restype = sz
+    lib.logo_cache_keep_capacity.argtypes = [PP, i32]
+    lib.logo_cache_keep_capacity.restype = i64
     lib.logo_status_str.argtypes = [ctypes.c_int]
     lib.logo_status_str.restype = ctypes.c_char_p
     lib.logo_version.restype = ctypes.c_char_p
@@ -181,6 +207,52 @@ class Problem:
                            ctypes.c_void_p(cu_seqlens.data_ptr()),
                            None if host is None else host.ctypes.data_as(ctypes.c_void_p),
                            num_q_heads, num_kv_heads, head_dim, self.window, self.softmax_scale)
+
+    @property
+    def c(self):
+        return ctypes.byref(self._c)
+
+
+class Prefix:
+    """Host description of the prefixes that groups of a problem's sequences
+    share (mirrors ``logo_prefix``): int32 device tensors ``cu_prefix`` [R+1]
+    (rows of the prefix tensors) and ``cu_group`` [R+1] (sequences), with
+    optional host copies used for the sizes and for validation."""
+
+    def __init__(self, cu_prefix, cu_group, *, total_tokens: Optional[int] = None,
+                 max_prefix: Optional[int] = None, max_group: Optional[int] = None,
+                 cu_prefix_host: Optional[Sequence[int]] = None,
+                 cu_group_host: Optional[Sequence[int]] = None):
+        import numpy as np
+
+        def host(x):
+            if x is None:
+                return None
+            return np.ascontiguousarray(np.asarray(x.cpu() if hasattr(x, "cpu") else x),
+                                        dtype=np.int32)
+
+        self.cu_prefix, self.cu_group = cu_prefix, cu_group
+        R = int(cu_prefix.numel()) - 1
+        if int(cu_group.numel()) - 1 != R:
+            raise ValueError("cu_prefix and cu_group: R + 1 entries each")
+        hp, hg = self._host_prefix, self._host_group = host(cu_prefix_host), host(cu_group_host)
+        for h, nm in ((hp, "cu_prefix_host"), (hg, "cu_group_host")):
+            if h is not None and h.size != R + 1:
+                raise ValueError(f"{nm}: R + 1 entries")
+        if hp is not None and R > 0:
+            total_tokens = int(hp[-1]) if total_tokens is None else total_tokens
+            max_prefix = int(np.max(np.diff(hp))) if max_prefix is None else max_prefix
+        if hg is not None and R > 0:
+            max_group = int(np.max(np.diff(hg))) if max_group is None else max_group
+        if None in (total_tokens, max_prefix, max_group):
+            raise ValueError("give total_tokens, max_prefix and max_group, or the host copies")
+        self.num_prefixes, self.total_tokens = R, int(total_tokens)
+        self.max_prefix, self.max_group = int(max_prefix), int(max_group)
+        self._c = _Prefix(R, self.total_tokens, self.max_prefix, self.max_group,
+                          ctypes.c_void_p(cu_prefix.data_ptr()),
+                          ctypes.c_void_p(cu_group.data_ptr()),
+                          None if hp is None else hp.ctypes.data_as(ctypes.c_void_p),
+                          None if hg is None else hg.ctypes.data_as(ctypes.c_void_p))
 
     @property
     def c(self):
@@ -729,6 +801,177 @@ def logo_decode_noalloc(prob: Problem, q, k, v, gate, out, *, threshold: Optiona
           _ptr(threshold_device), _ptr(gain_local), _ptr(gain_global), float(eps), _ptr(out),
           _ptr(active), _ptr(n_active), _stream())
     return out, active, n_active
+
+
+def _step_threshold(threshold, threshold_device):
+    """The mode of a decoding step for exactly one of the two thresholds."""
+    import torch
+    if (threshold is None) == (threshold_device is None):
+        raise ValueError("give exactly one of threshold / threshold_device")
+    if threshold_device is None:
+        return LOGO_SEL_THRESHOLD
+    if (threshold_device.dtype != torch.float32 or not threshold_device.is_cuda
+            or threshold_device.numel() < 1):
+        raise ValueError("threshold_device: device float32 tensor")
+    return LOGO_SEL_THRESHOLD_DEVICE
+
+
+def logo_decode_prefix_workspace_bytes(prob: Problem, prefix: Prefix) -> int:
+    return int(library().logo_decode_prefix_workspace_bytes(prob.c, prefix.c))
+
+
+def logo_decode_prefix(prob: Problem, prefix: Prefix, q, k_pre, v_pre, k, v, gate, *,
+                       threshold: Optional[float] = None, threshold_device=None, q_g=None,
+                       k_pre_g=None, v_pre_g=None, k_g=None, v_g=None, gain_local=None,
+                       gain_global=None, eps: float = 1e-6, out=None, active=None, n_active=None,
+                       ws=None):
+    """``logo_decode`` for sequences that share prefixes: the cache of a
+    sequence is its group's prefix (rows of ``k_pre`` / ``v_pre``
+    [prefix rows, Hkv, d]) followed by its own rows (``k`` / ``v``, bounded by
+    ``prob.cu_seqlens``; the last one is its new token).  Returns (out, active,
+    n_active), the last two None when not given."""
+    import torch
+    N, Hq, Hkv, d, B = (prob.total_tokens, prob.num_q_heads, prob.num_kv_heads, prob.head_dim,
+                        prob.num_seqs)
+    P = prefix.total_tokens
+    mode = _step_threshold(threshold, threshold_device)
+    _check(q, torch.bfloat16, (B, Hq, d), "q")
+    for t, nm, n in ((k_pre, "k_pre", P), (v_pre, "v_pre", P), (k, "k", N), (v, "v", N)):
+        _check(t, torch.bfloat16, (n, Hkv, d), nm)
+    for t, nm, shp in ((q_g, "q_g", (B, Hq, d)), (k_pre_g, "k_pre_g", (P, Hkv, d)),
+                       (v_pre_g, "v_pre_g", (P, Hkv, d)), (k_g, "k_g", (N, Hkv, d)),
+                       (v_g, "v_g", (N, Hkv, d))):
+        if t is not None:
+            _check(t, torch.bfloat16, shp, nm)
+    for t, nm in ((gain_local, "gain_local"), (gain_global, "gain_global")):
+        if t is not None:
+            _check(t, torch.float32, (Hq, d), nm)
+    _check(gate, torch.float32, (B,), "gate")
+    if out is None:
+        out = torch.empty((B, Hq, d), dtype=torch.bfloat16, device=q.device)
+    _check(out, torch.bfloat16, (B, Hq, d), "out")
+    if active is not None:
+        _check(active, torch.int32, (B,), "active")
+    if n_active is not None:
+        _check(n_active, torch.int32, (1,), "n_active")
+    if ws is None:
+        ws = torch.empty(logo_decode_prefix_workspace_bytes(prob, prefix), dtype=torch.uint8,
+                         device=q.device)
+    _call("logo_decode_prefix", prob.c, prefix.c, _ptr(q), _ptr(k_pre), _ptr(v_pre), _ptr(k),
+          _ptr(v), _ptr(q_g), _ptr(k_pre_g), _ptr(v_pre_g), _ptr(k_g), _ptr(v_g), _ptr(gate),
+          mode, float(threshold if threshold is not None else 0.0), _ptr(threshold_device),
+          _ptr(gain_local), _ptr(gain_global), float(eps), _ptr(out), _ptr(active),
+          _ptr(n_active), _ptr(ws), ws.numel(), _stream())
+    return out, active, n_active
+
+
+def _check_scores(prob: Problem, score_in, score, device):
+    """score_in as given (or None) and score, allocated when not given."""
+    import torch
+    shape = (prob.num_kv_heads, prob.total_tokens)
+    if score_in is not None:
+        _check(score_in, torch.float32, shape, "score_in")
+    if score is None:
+        score = torch.empty(shape, dtype=torch.float32, device=device)
+    return _check(score, torch.float32, shape, "score")
+
+
+def logo_cache_score(prob: Problem, q, k, *, sel_idx=None, cu_sel=None, lse=None, score_in=None,
+                     score=None, ws=None):
+    """The attention weight that every key received from the selected rows
+    (from every row without ``sel_idx`` / ``cu_sel``), fp32 [Hkv, N], added to
+    ``score_in`` (which may be ``score``).  ``lse`` [Hq, sel_idx.numel()] is
+    the forward's base-2 log-sum-exp; without it it is computed."""
+    import torch
+    N, Hq, Hkv, d = prob.total_tokens, prob.num_q_heads, prob.num_kv_heads, prob.head_dim
+    _check(q, torch.bfloat16, (N, Hq, d), "q")
+    _check(k, torch.bfloat16, (N, Hkv, d), "k")
+    if (sel_idx is None) != (cu_sel is None):
+        raise ValueError("give sel_idx and cu_sel together")
+    cap = N
+    if sel_idx is not None:
+        _check(sel_idx, torch.int32, None, "sel_idx")
+        _check(cu_sel, torch.int32, (prob.num_seqs + 1,), "cu_sel")
+        cap = sel_idx.numel()
+    if lse is not None:
+        _check(lse, torch.float32, (Hq, cap), "lse")
+    score = _check_scores(prob, score_in, score, q.device)
+    nbytes = 0
+    if lse is None:
+        ws, nbytes = _ws(prob, LOGO_ENTRY_CACHE_SCORE, cap, ws)
+    _call("logo_cache_score", prob.c, _ptr(q), _ptr(k), _ptr(sel_idx), _ptr(cu_sel), int(cap),
+          _ptr(lse), _ptr(score_in), _ptr(score), _ptr(ws), nbytes, _stream())
+    return score
+
+
+def logo_decode_score(prob: Problem, q, k, gate, *, threshold: Optional[float] = None,
+                      threshold_device=None, score_in=None, score=None, ws=None):
+    """The attention weight that each selected sequence's new token gives its
+    cached keys (arguments as for ``logo_decode``), fp32 [Hkv, N], added to
+    ``score_in`` (which may be ``score``)."""
+    import torch
+    N, Hq, Hkv, d, B = (prob.total_tokens, prob.num_q_heads, prob.num_kv_heads, prob.head_dim,
+                        prob.num_seqs)
+    mode = _step_threshold(threshold, threshold_device)
+    _check(q, torch.bfloat16, (B, Hq, d), "q")
+    _check(k, torch.bfloat16, (N, Hkv, d), "k")
+    _check(gate, torch.float32, (B,), "gate")
+    score = _check_scores(prob, score_in, score, q.device)
+    ws, nbytes = _ws(prob, LOGO_ENTRY_DECODE_SCORE, 0, ws)
+    _call("logo_decode_score", prob.c, _ptr(q), _ptr(k), _ptr(gate), mode,
+          float(threshold if threshold is not None else 0.0), _ptr(threshold_device),
+          _ptr(score_in), _ptr(score), _ptr(ws), nbytes, _stream())
+    return score
+
+
+def logo_cache_keep_capacity(prob: Problem, budget: int) -> int:
+    return int(library().logo_cache_keep_capacity(prob.c, int(budget)))
+
+
+def logo_cache_evict(prob: Problem, score, budget: int, *, recent: int = 0, k=None, v=None,
+                     k_g=None, v_g=None, k_out=None, v_out=None, k_g_out=None, v_g_out=None,
+                     score_out=None, keep_idx=None, cu_keep=None, ws=None) -> dict:
+    """Caches cut down to ``budget`` rows per sequence and KV head: the last
+    ``recent`` ones and those with the largest ``score`` [Hkv, N].  Outputs not
+    given are allocated with ``logo_cache_keep_capacity`` rows; given ones may
+    have more (the same number each).  Returns a dict of k_out, v_out, k_g_out,
+    v_g_out (None without their inputs), score_out, keep_idx and cu_keep."""
+    import torch
+    N, Hkv, d, B = prob.total_tokens, prob.num_kv_heads, prob.head_dim, prob.num_seqs
+    dev = prob.cu_seqlens.device
+    _check(score, torch.float32, (Hkv, N), "score")
+    cap = None
+    for t, dim in ((score_out, 1), (keep_idx, 1), (k_out, 0), (v_out, 0), (k_g_out, 0),
+                   (v_g_out, 0)):
+        if t is not None and cap is None:
+            cap = int(t.shape[dim])
+    if cap is None:
+        cap = max(logo_cache_keep_capacity(prob, budget), 0)
+    r = dict(k_out=k_out, v_out=v_out, k_g_out=k_g_out, v_g_out=v_g_out, score_out=score_out,
+             keep_idx=keep_idx, cu_keep=cu_keep)
+    for t, nm in ((k, "k"), (v, "v"), (k_g, "k_g"), (v_g, "v_g")):
+        o = nm + "_out"
+        if t is not None:
+            _check(t, torch.bfloat16, (N, Hkv, d), nm)
+            if r[o] is None:
+                r[o] = torch.empty((cap, Hkv, d), dtype=torch.bfloat16, device=dev)
+        if r[o] is not None:
+            _check(r[o], torch.bfloat16, (cap, Hkv, d), o)
+    if score_out is None:
+        r["score_out"] = torch.empty((Hkv, cap), dtype=torch.float32, device=dev)
+    if keep_idx is None:
+        r["keep_idx"] = torch.empty((Hkv, cap), dtype=torch.int32, device=dev)
+    if cu_keep is None:
+        r["cu_keep"] = torch.empty(B + 1, dtype=torch.int32, device=dev)
+    _check(r["score_out"], torch.float32, (Hkv, cap), "score_out")
+    _check(r["keep_idx"], torch.int32, (Hkv, cap), "keep_idx")
+    _check(r["cu_keep"], torch.int32, (B + 1,), "cu_keep")
+    ws, nbytes = _ws(prob, LOGO_ENTRY_CACHE_EVICT, 0, ws)
+    _call("logo_cache_evict", prob.c, _ptr(score), int(budget), int(recent), _ptr(k), _ptr(v),
+          _ptr(k_g), _ptr(v_g), _ptr(r["k_out"]), _ptr(r["v_out"]), _ptr(r["k_g_out"]),
+          _ptr(r["v_g_out"]), _ptr(r["score_out"]), _ptr(r["keep_idx"]), _ptr(r["cu_keep"]), cap,
+          _ptr(ws), nbytes, _stream())
+    return r
 
 
 def logo_gate_proj(x, w_g, out=None):

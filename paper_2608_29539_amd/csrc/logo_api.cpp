@@ -335,6 +335,160 @@ logo_status check_ws(void *ws, size_t ws_bytes, size_t need) {
     return LOGO_OK;
 }
 
+// --- the operators of shared and scored caches -------------------------------
+logo_status check_prefix(const logo_problem *p, const logo_prefix *x) {
+    if (!x || !x->cu_prefix || !x->cu_group)
+        return LOGO_ERR_NULL;
+    if (x->num_prefixes < 1 || x->total_tokens < 0 || x->max_prefix < 0 || x->max_group < 0 ||
+        x->max_group > p->num_seqs || (x->total_tokens > 0 && x->max_prefix < 1) ||
+        x->max_group < 1)
+        return LOGO_ERR_SHAPE;
+    const int R = x->num_prefixes;
+    if (x->cu_prefix_host) {
+        const int32_t *cu = x->cu_prefix_host;
+        if (cu[0] != 0 || cu[R] != x->total_tokens)
+            return LOGO_ERR_SHAPE;
+        for (int r = 0; r < R; r++) {
+            const long long n = (long long)cu[r + 1] - cu[r];
+            if (n < 0 || n > x->max_prefix)
+                return LOGO_ERR_SHAPE;
+        }
+    }
+    if (x->cu_group_host) {
+        const int32_t *cu = x->cu_group_host;
+        if (cu[0] != 0 || cu[R] != p->num_seqs)
+            return LOGO_ERR_SHAPE;
+        for (int r = 0; r < R; r++) {
+            const long long n = (long long)cu[r + 1] - cu[r];
+            if (n < 0 || n > x->max_group)
+                return LOGO_ERR_SHAPE;
+        }
+    }
+    // a cache without rows has no new token
+    if (x->cu_prefix_host && x->cu_group_host && p->cu_seqlens_host)
+        for (int r = 0; r < R; r++)
+            for (int b = x->cu_group_host[r]; b < x->cu_group_host[r + 1]; b++)
+                if (p->cu_seqlens_host[b + 1] == p->cu_seqlens_host[b] &&
+                    x->cu_prefix_host[r + 1] == x->cu_prefix_host[r])
+                    return LOGO_ERR_SHAPE;
+    // key positions and a tile's byte offsets are 32-bit
+    if ((long long)x->max_prefix + p->max_seqlen >= (1LL << 31) - kBlockN ||
+        (long long)p->num_kv_heads * p->head_dim * 2 * kBlockN >= (1LL << 31))
+        return LOGO_ERR_UNSUPPORTED;
+    return LOGO_OK;
+}
+
+struct PrefixPlan {
+    int pfx_tiles, own_tiles;
+    int kc[4], chunks[4], slot0[4], slots;
+    long long first[5];
+    size_t ml, total;
+};
+
+// Keys per chunk: the prefix's part of the global branch in about 512
+// workgroups (two per CU) over the KV heads and row tiles, at least 128 keys
+// each; the other ranges in chunks of 512 keys; at most kMaxPrefixChunks each.
+PrefixPlan prefix_plan(const logo_problem *p, const logo_prefix *x, bool share) {
+    PrefixPlan d;
+    const long long G = p->num_q_heads / p->num_kv_heads, w = p->window;
+    const long long maxP = x->max_prefix, maxS = p->max_seqlen;
+    d.pfx_tiles = (int)(((long long)x->max_group * G + kPrefixRows - 1) / kPrefixRows);
+    d.own_tiles = (int)((G + kPrefixRows - 1) / kPrefixRows);
+    const long long span[4] = {maxP, share ? (maxS > w ? maxS - w : 0) : maxS,
+                               maxP < w ? maxP : w, maxS < w ? maxS : w};
+    const long long work = (long long)x->total_tokens * p->num_kv_heads * d.pfx_tiles;
+    const long long want[4] = {std::max(128LL, (work + 511) / 512), 512, 512, 512};
+    long long slots = 0, first = 0;
+    for (int i = 0; i < 4; i++) {
+        long long kc = std::max(want[i], (span[i] + kMaxPrefixChunks - 1) / kMaxPrefixChunks);
+        kc = std::min((kc + kBlockN - 1) / kBlockN * kBlockN, (1LL << 31) - kBlockN);
+        d.kc[i] = (int)kc;
+        d.chunks[i] = (int)((span[i] + kc - 1) / kc);
+        d.slot0[i] = (int)slots;
+        slots += d.chunks[i];
+        const bool own = i & 1;
+        const long long pairs = (long long)(own ? p->num_seqs : x->num_prefixes) * d.chunks[i] *
+                                p->num_kv_heads;
+        d.first[i] = first;
+        first += (pairs + kQueues - 1) / kQueues * kQueues * (own ? d.own_tiles : d.pfx_tiles);
+    }
+    d.first[4] = first;
+    d.slots = (int)slots;
+    const size_t rows = (size_t)slots * p->num_seqs * p->num_q_heads;
+    d.ml = align_up(sizeof(float) * rows * p->head_dim);
+    d.total = d.ml + align_up(sizeof(float) * 2 * rows);
+    return d;
+}
+
+struct ScorePlan {
+    int key_waves, lse_kc, lse_chunks;
+    long long items, lse_items;
+    size_t lse, lse_part, total;
+};
+
+// Keys per workgroup (64, 128 or 256): the most that still makes 512
+// workgroups, two per CU.  Key chunks of the log-sum-exp likewise, of at least 256 keys.
+ScorePlan score_plan(const logo_problem *p, int32_t cap) {
+    ScorePlan d;
+    const long long N = p->total_tokens, B = p->num_seqs, H = p->num_kv_heads;
+    const long long G = p->num_q_heads / p->num_kv_heads;
+    d.key_waves = N * H >= 512 * 256 ? 4 : N * H >= 512 * 128 ? 2 : 1;
+    d.items = (N / (64 * d.key_waves) + B) * H;
+    const long long tiles = ((long long)cap * G) / kLseRows + B;
+    const long long maxL = std::max(1, p->max_seqlen);
+    long long chunks = std::min((512 + tiles * H - 1) / (tiles * H), (maxL + 255) / 256);
+    chunks = std::min(chunks, 64LL);
+    const long long kc = ((maxL + chunks - 1) / chunks + 63) / 64 * 64;
+    d.lse_kc = (int)std::min(kc, (1LL << 31) - 64);
+    d.lse_chunks = (int)((maxL + d.lse_kc - 1) / d.lse_kc);
+    d.lse_items = tiles * H * d.lse_chunks;
+    d.lse = 0;
+    d.lse_part = align_up(sizeof(float) * (size_t)cap * p->num_q_heads);
+    d.total = d.lse_part +
+              align_up(2 * sizeof(float) * (size_t)cap * p->num_q_heads * d.lse_chunks);
+    return d;
+}
+
+struct StepScorePlan {
+    int kc, chunks, out_chunks, head_blocks;
+    long long items, out_items;
+    size_t ml, total;
+};
+StepScorePlan step_score_plan(const logo_problem *p) {
+    StepScorePlan d;
+    const long long maxL = std::max(1, p->max_seqlen), B = p->num_seqs, H = p->num_kv_heads;
+    const long long G = p->num_q_heads / p->num_kv_heads;
+    d.head_blocks = (int)((G + 15) / 16);
+    d.kc = 512;
+    d.chunks = (int)((maxL + d.kc - 1) / d.kc);
+    d.out_chunks = (int)((maxL + kStepKeys - 1) / kStepKeys);
+    d.items = B * H * d.head_blocks * d.chunks;
+    d.out_items = B * H * d.out_chunks;
+    d.ml = align_up(sizeof(float) * (size_t)p->num_q_heads * p->total_tokens);
+    d.total = d.ml + align_up(2 * sizeof(float) * (size_t)B * p->num_q_heads * d.chunks);
+    return d;
+}
+
+int64_t keep_capacity(const logo_problem *p, int32_t budget) {
+    if (!p->cu_seqlens_host)
+        return std::min<int64_t>(p->total_tokens, (int64_t)p->num_seqs * budget);
+    int64_t s = 0;
+    for (int b = 0; b < p->num_seqs; b++)
+        s += std::min(p->cu_seqlens_host[b + 1] - p->cu_seqlens_host[b], budget);
+    return s;
+}
+
+bool misaligned(const void *p) { return ((uintptr_t)p % 16) != 0; }
+
+// The threshold of a decoding step (host value or device scalar).
+logo_status check_step_threshold(logo_sel_mode mode, float threshold, const float *thr_dev) {
+    if (mode == LOGO_SEL_THRESHOLD)
+        return std::isnan(threshold) ? LOGO_ERR_ARG : LOGO_OK;
+    if (mode == LOGO_SEL_THRESHOLD_DEVICE)
+        return thr_dev ? LOGO_OK : LOGO_ERR_NULL;
+    return LOGO_ERR_ARG;
+}
+
 int64_t ratio_capacity(const logo_problem *p, double ratio) {
     if (!p->cu_seqlens_host)
         return p->total_tokens;
@@ -941,6 +1095,9 @@ size_t logo_workspace_bytes(const logo_problem *p, int entry, int32_t sel_capaci
     case LOGO_ENTRY_BWD: return bwd_ws(p, cap).total;
     case LOGO_ENTRY_DENSE_BWD: return dense_bwd_ws(p);
     case LOGO_ENTRY_GLOBAL_BWD: return global_bwd_ws(p, cap).total;
+    case LOGO_ENTRY_CACHE_SCORE: return score_plan(p, cap).total;
+    case LOGO_ENTRY_DECODE_SCORE: return step_score_plan(p).total;
+    case LOGO_ENTRY_CACHE_EVICT:
     case LOGO_ENTRY_LOCAL:
     case LOGO_ENTRY_COMBINE:
     case LOGO_ENTRY_DENSE: return 0;
@@ -1572,6 +1729,273 @@ logo_status logo_global_attn_sparse_q_bwd(const logo_problem *p, const logo_bf16
     if (st == LOGO_OK)
         st = hip_status(launch_bwd_dkv(kModeGlobal, d, a, (int)grid_kv, s), s);
     return st;
+}
+
+size_t logo_decode_prefix_workspace_bytes(const logo_problem *p, const logo_prefix *prefix) {
+    if (check_problem(p) != LOGO_OK || check_prefix(p, prefix) != LOGO_OK)
+        return 0;
+    // (the branches' own tensors make more chunks)
+    return std::max(prefix_plan(p, prefix, false).total, prefix_plan(p, prefix, true).total);
+}
+
+logo_status logo_decode_prefix(const logo_problem *p, const logo_prefix *prefix,
+                               const logo_bf16 *q, const logo_bf16 *k_pre, const logo_bf16 *v_pre,
+                               const logo_bf16 *k, const logo_bf16 *v, const logo_bf16 *q_g,
+                               const logo_bf16 *k_pre_g, const logo_bf16 *v_pre_g,
+                               const logo_bf16 *k_g, const logo_bf16 *v_g, const float *gate,
+                               logo_sel_mode mode, float threshold, const float *thr_dev,
+                               const float *gain_local, const float *gain_global, float eps,
+                               logo_bf16 *out, int32_t *active, int32_t *n_active, void *ws,
+                               size_t ws_bytes, logo_stream stream) {
+    logo_status st = check_problem(p);
+    if (st == LOGO_OK)
+        st = check_prefix(p, prefix);
+    if (st != LOGO_OK)
+        return st;
+    if (!q || !gate || !out || (p->total_tokens > 0 && (!k || !v)) ||
+        (prefix->total_tokens > 0 && (!k_pre || !v_pre)))
+        return LOGO_ERR_NULL;
+    if ((st = check_step_threshold(mode, threshold, thr_dev)) != LOGO_OK)
+        return st;
+    if (!(eps >= 0.f) || std::isinf(eps))
+        return LOGO_ERR_ARG;
+    // a cache is one tensor pair: keys and values of both its parts, or none
+    if ((k_g == nullptr) != (v_g == nullptr) || (k_pre_g == nullptr) != (v_pre_g == nullptr) ||
+        (p->total_tokens > 0 && prefix->total_tokens > 0 &&
+         (k_g == nullptr) != (k_pre_g == nullptr)))
+        return LOGO_ERR_ARG;
+    const void *rows[] = {q, k_pre, v_pre, k, v, q_g, k_pre_g, v_pre_g, k_g, v_g, out};
+    for (const void *x : rows)
+        if (misaligned(x))
+            return LOGO_ERR_ARG;
+    if ((long long)p->num_seqs * p->num_q_heads >= (1LL << 31))
+        return LOGO_ERR_UNSUPPORTED;
+    PrefixArgs a;
+    std::memset(&a, 0, sizeof a);
+    a.q = q;
+    a.k = k;
+    a.v = v;
+    a.kp = k_pre;
+    a.vp = v_pre;
+    a.q_g = q_g ? q_g : q;
+    a.k_g = k_g ? k_g : k;
+    a.v_g = v_g ? v_g : v;
+    a.kp_g = k_pre_g ? k_pre_g : k_pre;
+    a.vp_g = v_pre_g ? v_pre_g : v_pre;
+    a.share = a.q_g == q && a.k_g == k && a.v_g == v && a.kp_g == k_pre && a.vp_g == v_pre;
+    const PrefixPlan d = prefix_plan(p, prefix, a.share);
+    if (d.first[4] >= (1LL << 31) - 1)
+        return LOGO_ERR_UNSUPPORTED;
+    if ((st = check_ws(ws, ws_bytes, d.total)) != LOGO_OK)
+        return st;
+    a.cu = p->cu_seqlens;
+    a.cu_pre = prefix->cu_prefix;
+    a.cu_grp = prefix->cu_group;
+    a.gate = gate;
+    a.gain_local = gain_local;
+    a.gain_global = gain_global;
+    a.eps = eps;
+    a.scale_log2 = scale_log2(p);
+    a.num_seqs = p->num_seqs;
+    a.num_prefixes = prefix->num_prefixes;
+    a.hq = p->num_q_heads;
+    a.hkv = p->num_kv_heads;
+    a.group = p->num_q_heads / p->num_kv_heads;
+    a.head_dim = p->head_dim;
+    a.window = p->window;
+    a.pfx_tiles = d.pfx_tiles;
+    a.own_tiles = d.own_tiles;
+    for (int i = 0; i < 4; i++) {
+        a.kc[i] = d.kc[i];
+        a.chunks[i] = d.chunks[i];
+        a.slot0[i] = d.slot0[i];
+    }
+    for (int i = 0; i < 5; i++)
+        a.first[i] = (int32_t)d.first[i];
+    a.act = active;
+    a.n_act = n_active;
+    a.sel_mode = (int32_t)mode;
+    a.thr_host = threshold;
+    a.thr_dev = thr_dev;
+    a.part = (float *)ws;
+    a.ml = (float *)((char *)ws + d.ml);
+    a.out = out;
+    hipStream_t s = (hipStream_t)stream;
+    return hip_status(launch_decode_prefix(a, s), s);
+}
+
+logo_status logo_cache_score(const logo_problem *p, const logo_bf16 *q, const logo_bf16 *k,
+                             const int32_t *sel_idx, const int32_t *cu_sel, int32_t sel_capacity,
+                             const float *lse, const float *score_in, float *score, void *ws,
+                             size_t ws_bytes, logo_stream stream) {
+    logo_status st = check_problem(p);
+    if (st != LOGO_OK)
+        return st;
+    if (sel_capacity < 0)
+        return LOGO_ERR_SHAPE;
+    if ((sel_idx == nullptr) != (cu_sel == nullptr) && !(cu_sel && sel_capacity == 0))
+        return LOGO_ERR_NULL;
+    const int32_t N = p->total_tokens;
+    if (N > 0 && (!q || !k || !score))
+        return LOGO_ERR_NULL;
+    if (misaligned(q) || misaligned(k))
+        return LOGO_ERR_ARG;
+    if (N == 0)
+        return LOGO_OK;
+    const int32_t cap = cu_sel ? sel_capacity : N;
+    if ((long long)cap * p->num_q_heads >= (1LL << 31))
+        return LOGO_ERR_UNSUPPORTED;
+    const ScorePlan d = score_plan(p, cap);
+    if (d.items >= (1LL << 31) || d.lse_items >= (1LL << 31))
+        return LOGO_ERR_UNSUPPORTED;
+    if (!lse && cap > 0 && (st = check_ws(ws, ws_bytes, d.total)) != LOGO_OK)
+        return st;
+    ScoreArgs a;
+    std::memset(&a, 0, sizeof a);
+    a.q = q;
+    a.k = k;
+    a.cu = p->cu_seqlens;
+    a.sel_idx = sel_idx;
+    a.cu_sel = cu_sel;
+    a.lse = lse;
+    if (!lse && cap > 0) {
+        a.lse_out = (float *)((char *)ws + d.lse);
+        a.lse_part = (float *)((char *)ws + d.lse_part);
+        a.lse = a.lse_out;
+    }
+    a.score_in = score_in;
+    a.score = score;
+    a.n = N;
+    a.cap = cap;
+    a.num_seqs = p->num_seqs;
+    a.hq = p->num_q_heads;
+    a.hkv = p->num_kv_heads;
+    a.group = p->num_q_heads / p->num_kv_heads;
+    a.head_dim = p->head_dim;
+    a.scale_log2 = scale_log2(p);
+    a.key_waves = d.key_waves;
+    a.items = (int32_t)d.items;
+    a.lse_kc = d.lse_kc;
+    a.lse_chunks = d.lse_chunks;
+    a.lse_items = (int32_t)d.lse_items;
+    hipStream_t s = (hipStream_t)stream;
+    return hip_status(launch_cache_score(a, s), s);
+}
+
+logo_status logo_decode_score(const logo_problem *p, const logo_bf16 *q, const logo_bf16 *k,
+                              const float *gate, logo_sel_mode mode, float threshold,
+                              const float *thr_dev, const float *score_in, float *score, void *ws,
+                              size_t ws_bytes, logo_stream stream) {
+    logo_status st = check_problem(p);
+    if (st != LOGO_OK)
+        return st;
+    const int32_t N = p->total_tokens;
+    if (N > 0 && (!q || !k || !gate || !score))
+        return LOGO_ERR_NULL;
+    if ((st = check_step_threshold(mode, threshold, thr_dev)) != LOGO_OK)
+        return st;
+    if (misaligned(q) || misaligned(k))
+        return LOGO_ERR_ARG;
+    if (p->cu_seqlens_host)
+        for (int b = 0; b < p->num_seqs; b++)
+            if (p->cu_seqlens_host[b + 1] - p->cu_seqlens_host[b] < 1)
+                return LOGO_ERR_SHAPE;
+    if (N == 0)
+        return LOGO_OK;
+    const StepScorePlan d = step_score_plan(p);
+    if (d.items >= (1LL << 31) || d.out_items >= (1LL << 31) ||
+        (long long)p->num_seqs * p->num_q_heads >= (1LL << 31) ||
+        p->num_q_heads / p->num_kv_heads > 8192)
+        return LOGO_ERR_UNSUPPORTED;
+    if ((st = check_ws(ws, ws_bytes, d.total)) != LOGO_OK)
+        return st;
+    StepScoreArgs a;
+    std::memset(&a, 0, sizeof a);
+    a.q = q;
+    a.k = k;
+    a.cu = p->cu_seqlens;
+    a.gate = gate;
+    a.score_in = score_in;
+    a.score = score;
+    a.logits = (float *)ws;
+    a.ml = (float *)((char *)ws + d.ml);
+    a.n = N;
+    a.num_seqs = p->num_seqs;
+    a.hq = p->num_q_heads;
+    a.hkv = p->num_kv_heads;
+    a.group = p->num_q_heads / p->num_kv_heads;
+    a.head_dim = p->head_dim;
+    a.head_blocks = d.head_blocks;
+    a.scale_log2 = scale_log2(p);
+    a.kc = d.kc;
+    a.chunks = d.chunks;
+    a.items = (int32_t)d.items;
+    a.out_chunks = d.out_chunks;
+    a.out_items = (int32_t)d.out_items;
+    a.sel_mode = (int32_t)mode;
+    a.thr_host = threshold;
+    a.thr_dev = thr_dev;
+    hipStream_t s = (hipStream_t)stream;
+    return hip_status(launch_decode_score(a, s), s);
+}
+
+int64_t logo_cache_keep_capacity(const logo_problem *p, int32_t budget) {
+    if (check_problem(p) != LOGO_OK || budget < 1)
+        return -1;
+    return keep_capacity(p, budget);
+}
+
+logo_status logo_cache_evict(const logo_problem *p, const float *score, int32_t budget,
+                             int32_t recent, const logo_bf16 *k, const logo_bf16 *v,
+                             const logo_bf16 *k_g, const logo_bf16 *v_g, logo_bf16 *k_out,
+                             logo_bf16 *v_out, logo_bf16 *k_g_out, logo_bf16 *v_g_out,
+                             float *score_out, int32_t *keep_idx, int32_t *cu_keep,
+                             int32_t capacity, void *ws, size_t ws_bytes,
+                             logo_stream stream) {
+    logo_status st = check_problem(p);
+    if (st != LOGO_OK)
+        return st;
+    if (!cu_keep)
+        return LOGO_ERR_NULL;
+    if (budget < 1 || recent < 0)
+        return LOGO_ERR_ARG;
+    const logo_bf16 *in[4] = {k, v, k_g, v_g};
+    logo_bf16 *out[4] = {k_out, v_out, k_g_out, v_g_out};
+    for (int i = 0; i < 4; i++) {
+        if ((in[i] == nullptr) != (out[i] == nullptr) ||
+            (in[i] == nullptr) != (in[i ^ 1] == nullptr) || misaligned(in[i]) ||
+            misaligned(out[i]))
+            return LOGO_ERR_ARG;
+    }
+    if (p->total_tokens > 0 && (!score || !score_out || !keep_idx))
+        return LOGO_ERR_NULL;
+    if (capacity < keep_capacity(p, budget))
+        return LOGO_ERR_SHAPE;
+    if ((long long)p->num_seqs * p->num_kv_heads >= (1LL << 31) ||
+        (long long)capacity * p->num_kv_heads * (p->head_dim / 8) / 256 >= (1LL << 31) - 1)
+        return LOGO_ERR_UNSUPPORTED;
+    (void)ws;                                    // (none needed)
+    (void)ws_bytes;
+    EvictArgs a;
+    std::memset(&a, 0, sizeof a);
+    a.score = score;
+    a.cu = p->cu_seqlens;
+    a.n = p->total_tokens;
+    a.num_seqs = p->num_seqs;
+    a.hkv = p->num_kv_heads;
+    a.head_dim = p->head_dim;
+    a.budget = budget;
+    a.recent = recent;
+    a.cap = capacity;
+    for (int i = 0; i < 4; i++) {
+        a.in[i] = in[i];
+        a.out[i] = out[i];
+    }
+    a.score_out = score_out;
+    a.keep_idx = keep_idx;
+    a.cu_keep = cu_keep;
+    hipStream_t s = (hipStream_t)stream;
+    return hip_status(launch_cache_evict(a, s), s);
 }
 
 }  // extern "C"
