@@ -7,7 +7,8 @@
 // to the same key; every sum is taken in a fixed order, so results do not
 // change from run to run.
 //
-//   score_lse_kernel, score_lse_join_kernel   lse where the caller has none
+//   score_lse_kernel        (m, l) of the rows by chunks of keys, where the
+//                           caller has no lse
 //   score_kernel            key-stationary: a wave keeps 64 keys of one KV head
 //                           in registers (the MFMA's B operand) and walks over
 //                           the rows that see them, so a key's sum stays in
@@ -15,16 +16,18 @@
 //   step_logits_kernel      one query per sequence: the scaled scores of a
 //                           chunk of keys and their (m, l) per head
 //   step_weights_kernel     2^(score - lse) summed over the heads
-#include "attn_common.h"
+#include "attn_tiles.h"
 #include "decode_common.h"
 #include "logo_internal.h"
+
+#include <type_traits>
 
 namespace logo {
 namespace {
 
 constexpr int kScoreThreads = 256;
 constexpr int kScoreWaves = kScoreThreads / 64;
-constexpr int kRowPad = 8;                  // bf16 of padding per staged row (bank offset)
+constexpr int kLseBuffers = 4;
 
 // Item t of the blocks that sequences have n(b) of each, sequence-major: its
 // sequence and block; false past the last.  Every wave searches for itself.
@@ -81,11 +84,11 @@ __device__ __forceinline__ f32x16 block_scores(const uint16_t *frag, const bf16x
 
 // ---------------------------------------------------------------------------
 // lse of the query rows.  Workgroup: 128 flattened (rank, head) rows of one
-// sequence and KV head x a chunk of keys, 64 keys staged at a time.
+// sequence and KV head x a chunk of keys.
 // ---------------------------------------------------------------------------
 template <int D>
-__global__ __launch_bounds__(kScoreThreads) void score_lse_kernel(const ScoreArgs a) {
-    __shared__ __attribute__((aligned(16))) uint16_t s_k[2][64][D + kRowPad];
+__global__ __launch_bounds__(kScoreThreads, 2) void score_lse_kernel(const ScoreArgs a) {
+    __shared__ __attribute__((aligned(16))) uint16_t s_k[kLseBuffers][kBlockN][D + kKPad];
     const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6);
     const int g = lane >> 5, m = lane & 31;
     const int G = a.group;
@@ -121,118 +124,128 @@ __global__ __launch_bounds__(kScoreThreads) void score_lse_kernel(const ScoreArg
     for (int s = 0; s < D / 16; s++)
         qf[s] = *(const bf16x8 *)(qp + s * 16);
 
-    // 64 keys x D: each thread D / 32 pieces of 8
-    constexpr int kPieces = 64 * D / 8 / kScoreThreads;
+    // K tiles of 64 keys in four buffers, loaded three tiles ahead.  (A wave
+    // issues kPerWaveK or one less loads per tile; counting the smaller number
+    // as pending waits for no less than is needed.)
+    constexpr int kAhead = kLseBuffers - 1;
+    constexpr int kLoads = Dma<D, kScoreWaves>::kInstK / kScoreWaves;
+    const int row_bytes = a.hkv * D * 2;
     const uint16_t *kb = a.k + (base * a.hkv + kvh) * (int64_t)D;
-    u32x4 reg[kPieces];
-    auto load = [&](int key) {
-#pragma unroll
-        for (int i = 0; i < kPieces; i++) {
-            const int x = tid + i * kScoreThreads, row = x / (D / 8), col = x % (D / 8);
-            reg[i] = key + row < k1
-                         ? *(const u32x4 *)(kb + (int64_t)(key + row) * a.hkv * D + col * 8)
-                         : u32x4{};
-        }
+    Dma<D, kScoreWaves> dma;
+    dma_plan<D, kScoreWaves>(dma, wave, lane, row_bytes);
+    auto stage = [&](int key, int buf) {
+        if (key < k1)
+            dma_k<D, kScoreWaves>(&s_k[buf][0][0], dma, kb, k1, key, row_bytes, wave);
     };
-    auto put = [&](int buf) {
 #pragma unroll
-        for (int i = 0; i < kPieces; i++) {
-            const int x = tid + i * kScoreThreads, row = x / (D / 8), col = x % (D / 8);
-            *(u32x4 *)&s_k[buf][row][col * 8] = reg[i];
-        }
-    };
+    for (int i = 0; i < kAhead; i++)
+        stage(k0 + i * kBlockN, i);
     const bool live = wave * 32 < nrows;
     float mr = kNegInf, l = 0.f;
-    load(k0);
-    put(0);
     int buf = 0;
-    for (int key = k0; key < k1; key += 64, buf ^= 1) {
-        __syncthreads();
-        const bool more = key + 64 < k1;
-        if (more)
-            load(key + 64);
-        if (live) {
-            f32x16 s[2];
+    for (int key = k0; key < k1; key += kBlockN, buf = (buf + 1) % kLseBuffers) {
+        if (key + (kAhead - 1) * kBlockN < k1)
+            dma_wait_barrier_but<(kAhead - 1) * kLoads>();
+        else
+            dma_wait_barrier();
+        stage(key + kAhead * kBlockN, (buf + kAhead) % kLseBuffers);
+        if (!live)
+            continue;
+        f32x16 s[2];
 #pragma unroll
-            for (int sb = 0; sb < 2; sb++)
-                s[sb] = block_scores<D>(&s_k[buf][sb * 32 + m][g * 8], qf);
-            if (key + 63 > pos_min || key + 64 > k1) {
-#pragma unroll
-                for (int sb = 0; sb < 2; sb++)
-#pragma unroll
-                    for (int i = 0; i < 16; i++) {
-                        const int j = key + sb * 32 + (i >> 2) * 8 + g * 4 + (i & 3);
-                        if (j > pos || j >= k1)
-                            s[sb][i] = kNegInf;
-                    }
-            }
-            float mx = kNegInf;
+        for (int sb = 0; sb < 2; sb++)
+            s[sb] = block_scores<D>(&s_k[buf][sb * 32 + m][g * 8], qf);
+        if (key + 63 > pos_min || key + 64 > k1) {
 #pragma unroll
             for (int sb = 0; sb < 2; sb++)
 #pragma unroll
-                for (int i = 0; i < 16; i++)
-                    mx = fmaxf(mx, s[sb][i]);
-            mx = pair_max(mx) * a.scale_log2;
-            const float mn = fmaxf(mr, mx), mc = mn == kNegInf ? 0.f : mn;
-            float sum = 0.f;
-#pragma unroll
-            for (int sb = 0; sb < 2; sb++)
-#pragma unroll
-                for (int i = 0; i < 16; i++)
-                    sum += __builtin_amdgcn_exp2f(fmaf(s[sb][i], a.scale_log2, -mc));
-            l = fmaf(l, __builtin_amdgcn_exp2f(mr - mc), sum);
-            mr = mn;
+                for (int i = 0; i < 16; i++) {
+                    const int j = key + sb * 32 + (i >> 2) * 8 + g * 4 + (i & 3);
+                    if (j > pos || j >= k1)
+                        s[sb][i] = kNegInf;
+                }
         }
-        if (more)
-            put(buf ^ 1);
+        float mx = kNegInf;
+#pragma unroll
+        for (int sb = 0; sb < 2; sb++)
+#pragma unroll
+            for (int i = 0; i < 16; i++)
+                mx = fmaxf(mx, s[sb][i]);
+        mx = pair_max(mx) * a.scale_log2;
+        const float mn = fmaxf(mr, mx), mc = mn == kNegInf ? 0.f : mn;
+        float sum = 0.f;
+#pragma unroll
+        for (int sb = 0; sb < 2; sb++)
+#pragma unroll
+            for (int i = 0; i < 16; i++)
+                sum += __builtin_amdgcn_exp2f(fmaf(s[sb][i], a.scale_log2, -mc));
+        l = fmaf(l, __builtin_amdgcn_exp2f(mr - mc), sum);
+        mr = mn;
     }
     l = pair_sum(l);
     if (live && wave * 32 + m < nrows && g == 0)
         *(f32x2 *)(a.lse_part + (((int64_t)c * a.hq + head) * a.cap + rank) * 2) = f32x2{mr, l};
 }
 
-// lse[head][rank] from the chunks' (m, l); chunks past the row's position
-// were not written.
-__global__ __launch_bounds__(256) void score_lse_join_kernel(const ScoreArgs a) {
-    const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int rank = (int)(x % a.cap), head = (int)(x / a.cap);
-    if (head >= a.hq || (a.sel_idx && rank >= a.cu_sel[a.num_seqs]))
-        return;
-    const int64_t tok = token_of(a, rank);
-    int lo = 0, hi = a.num_seqs - 1;             // the token's sequence
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (a.cu[mid] <= tok)
-            lo = mid;
-        else
-            hi = mid - 1;
-    }
-    const int n = min((int)(tok - a.cu[lo]) / a.lse_kc + 1, a.lse_chunks);
-    float M = kNegInf, l = 0.f;
-    for (int c = 0; c < n; c++) {
-        const f32x2 v = *(const f32x2 *)(a.lse_part + (((int64_t)c * a.hq + head) * a.cap + rank) * 2);
-        const float mn = fmaxf(M, v[0]), mc = mn == kNegInf ? 0.f : mn;
-        l = l * __builtin_amdgcn_exp2f(M - mc) + v[1] * __builtin_amdgcn_exp2f(v[0] - mc);
-        M = mn;
-    }
-    a.lse_out[(int64_t)head * a.cap + rank] = M + __builtin_amdgcn_logf(l);
-}
-
 // ---------------------------------------------------------------------------
 // The weights' sums.  Workgroup: KW x 64 keys of one sequence and KV head (KW
-// waves side by side, 4 / KW rows of waves); the rows that see them are staged
-// kScoreRows at a time, and each row of waves takes its share.
+// waves side by side, 4 / KW rows of waves).  The rows that see them pass
+// through LDS, kScoreRows at a time in two buffers filled by direct loads: a
+// step has the next one's rows on their way while it multiplies its own, and
+// the addresses, positions and lse of the one after that, so that a step waits
+// for no chain of loads.  A row's 16-byte pieces are permuted (piece c of row r
+// is at c ^ (r % pieces)) so that the fragment reads of 16 rows hit distinct
+// banks.  Each Q fragment feeds two products (the wave's two blocks of 32
+// keys), and the exponentials of one block of rows are issued between the
+// products of the next.
 // ---------------------------------------------------------------------------
 constexpr int kScoreRows = 128;
 
+// One 16-byte-per-lane load from a lane's own address to LDS (lane i writes
+// the 16 bytes at lds + 16 i); see lds_load16_at.
+__device__ __forceinline__ void lds_gather16(const void *src, uint32_t lds) {
+    const uint32_t lds_addr = __builtin_amdgcn_readfirstlane(lds);
+    uint32_t saved;
+    asm volatile(
+        "s_mov_b32 %0, m0\n\t"
+        "s_mov_b32 m0, %1\n\t"
+        "s_nop 0\n\t"
+        "global_load_lds_dwordx4 %2, off\n\t"
+        "s_mov_b32 m0, %0"
+        : "=&s"(saved)
+        : "s"(lds_addr), "v"(src)
+        : "memory");
+}
+
+// First rank in [lo, hi) whose token is at or past `tok` (tokens ascend):
+// every lane probes one of 64 equally spaced ranks.
+__device__ __forceinline__ int first_rank(const ScoreArgs &a, int lo, int hi, int tok) {
+    if (!a.sel_idx)
+        return min(max(tok, lo), hi);
+    const int lane = threadIdx.x & 63;
+    while (lo < hi) {
+        const int step = (hi - lo + 63) >> 6;
+        const int64_t at = lo + (int64_t)lane * step;
+        const int n = (int)__popcll(__ballot(at < hi && a.sel_idx[at] < tok));
+        if (n == 0)
+            break;
+        const int64_t end = lo + (int64_t)n * step;
+        lo += (n - 1) * step + 1;
+        hi = (int)min((int64_t)hi, end);
+    }
+    return uni(lo);
+}
+
 template <int D, int KW>
 __global__ __launch_bounds__(kScoreThreads, 2) void score_kernel(const ScoreArgs a) {
+    constexpr int R = kScoreRows;
     constexpr int RW = kScoreWaves / KW;         // waves that share their keys
-    constexpr int kBlocks = kScoreRows / 32 / RW;   // row blocks per wave and step
-    __shared__ __attribute__((aligned(16))) uint16_t s_q[kScoreRows][D + kRowPad];
-    __shared__ __attribute__((aligned(16))) float s_lse[kScoreRows];
-    __shared__ __attribute__((aligned(16))) int s_pos[kScoreRows];
-    __shared__ float s_sum[RW][KW * 64];
+    constexpr int kBlocks = R / 32 / RW;         // row blocks per wave and step
+    constexpr int kPc = D / 8;                   // 16-byte pieces of a row
+    __shared__ __attribute__((aligned(16))) uint16_t s_q[2][R * D];
+    __shared__ __attribute__((aligned(16))) float s_lse[3][R];
+    __shared__ __attribute__((aligned(16))) int s_pos[3][R];
+    __shared__ const uint16_t *s_row[3][R];
     const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6);
     const int g = lane >> 5, m = lane & 31;
     const int kw = wave % KW, rw = wave / KW;
@@ -242,106 +255,185 @@ __global__ __launch_bounds__(kScoreThreads, 2) void score_kernel(const ScoreArgs
     if (!find_block(blockIdx.x / a.hkv, a.num_seqs,
                     [&](int i) { return (a.cu[i + 1] - a.cu[i] + KW * 64 - 1) / (KW * 64); }, b, jb))
         return;
-    const int64_t base = a.cu[b];
-    const int T = a.cu[b + 1] - (int)base;
+    const int base = a.cu[b];
+    const int T = a.cu[b + 1] - base;
     const int key0 = jb * KW * 64, my0 = key0 + kw * 64;
-    // the rows that see key0: from the first of position >= key0
-    int s0, s1;
-    row_span(a, b, s0, s1);
-    {
-        int hi = s1;
-        while (s0 < hi) {
-            const int mid = s0 + ((hi - s0) >> 1);
-            if (token_of(a, mid) - base < key0)
-                s0 = mid + 1;
-            else
-                hi = mid;
-        }
-    }
-    const int64_t rows = (int64_t)(s1 - s0) * G;
-
     // this wave's keys
     bf16x8 kf[2][D / 16];
 #pragma unroll
     for (int kb = 0; kb < 2; kb++) {
         const int key = my0 + kb * 32 + m;
-        const uint16_t *kp = a.k + ((base + key) * a.hkv + kvh) * (int64_t)D + g * 8;
+        const uint16_t *kp = a.k + ((int64_t)(base + key) * a.hkv + kvh) * D + g * 8;
 #pragma unroll
         for (int s = 0; s < D / 16; s++)
             kf[kb][s] = key < T ? *(const bf16x8 *)(kp + s * 16) : bf16x8{};
     }
-    float sum[2] = {0.f, 0.f};
+    // the rows that see key0 (a row is a rank and one of the G heads)
+    int s0, s1;
+    row_span(a, b, s0, s1);
+    s0 = first_rank(a, s0, s1, base + key0);
+    const int rows = (s1 - s0) * G;              // (cap * Hq < 2^31 - 1024)
+    const int steps = (rows + R - 1) / R;
 
-    for (int64_t r0 = 0; r0 < rows; r0 += kScoreRows) {
-        const int nrows = (int)(rows - r0 < kScoreRows ? rows - r0 : kScoreRows);
-        __syncthreads();                         // the last step's rows are read
-        constexpr int kPieces = kScoreRows * D / 8 / kScoreThreads;
-#pragma unroll
-        for (int i = 0; i < kPieces; i++) {
-            const int x = tid + i * kScoreThreads, row = x / (D / 8), col = x % (D / 8);
-            u32x4 v = {};
-            if (row < nrows) {
-                const int64_t flat = r0 + row;
-                const int64_t tok = token_of(a, s0 + (int)(flat / G));
-                v = *(const u32x4 *)(a.q + (tok * a.hq + kvh * G + flat % G) * D + col * 8);
-            }
-            *(u32x4 *)&s_q[row][col * 8] = v;
-        }
-        if (tid < kScoreRows) {
-            float lse = 0.f;
-            int pos = -1;                        // rows past the last see nothing
-            if (tid < nrows) {
-                const int64_t flat = r0 + tid;
-                const int rank = s0 + (int)(flat / G);
-                lse = a.lse[(int64_t)(kvh * G + flat % G) * a.cap + rank];
-                pos = (int)(token_of(a, rank) - base);
-            }
-            s_lse[tid] = lse;
-            s_pos[tid] = pos;
-        }
-        __syncthreads();
+    // Row tid / kSub of a step: kSub threads each, which join the key chunks
+    // of a row whose lse is not given.  Rows past the last have the last one's
+    // address and see nothing.
+    constexpr int kSub = kScoreThreads / R;
+    struct Meta {
+        const uint16_t *row;
+        float lse;
+        int pos;
+    };
+    auto meta_load = [&](int step) {
+        Meta x;
+        const int flat = step * R + tid / kSub, f = min(flat, rows - 1);
+        const int rank = s0 + f / G, head = kvh * G + f % G;
+        const int tok = token_of(a, rank);
+        x.pos = flat < rows ? tok - base : -1;
+        x.row = a.q + ((int64_t)tok * a.hq + head) * D;
+        if (!a.lse_part) {
+            x.lse = a.lse[(int64_t)head * a.cap + rank];
+        } else {
+            const int n = min((tok - base) / a.lse_kc + 1, a.lse_chunks);
+            const f32x2 *pp = (const f32x2 *)a.lse_part + (int64_t)head * a.cap + rank;
+            const int64_t stride = (int64_t)a.hq * a.cap;
+            float M = kNegInf, l = 0.f;
 #pragma unroll 1
-        for (int x = 0; x < kBlocks; x++) {
-            const int rb = x * RW + rw;          // 32-row block of the staged rows
-            // rows ascend: the first one's position bounds what all see, and
-            // the last block may have rows past the end
-            const bool masked = uni(s_pos[rb * 32]) < my0 + 63 || (rb + 1) * 32 > nrows;
+            for (int c = tid % kSub; c < n; c += 4 * kSub) {
+                f32x2 v[4];
 #pragma unroll
-            for (int kb = 0; kb < 2; kb++) {
-                const f32x16 s = block_scores<D>(&s_q[rb * 32 + m][g * 8], kf[kb]);
-                const int key = my0 + kb * 32 + m;
-                float part = 0.f;
+                for (int i = 0; i < 4; i++)
+                    v[i] = c + i * kSub < n ? pp[(c + i * kSub) * stride] : f32x2{kNegInf, 0.f};
+                const float mn = fmaxf(fmaxf(fmaxf(v[0][0], v[1][0]), fmaxf(v[2][0], v[3][0])), M);
+                const float mc = mn == kNegInf ? 0.f : mn;
+                l *= __builtin_amdgcn_exp2f(M - mc);
 #pragma unroll
-                for (int q = 0; q < 4; q++) {
-                    const f32x4 ls = *(const f32x4 *)&s_lse[rb * 32 + q * 8 + g * 4];
+                for (int i = 0; i < 4; i++)
+                    l = fmaf(v[i][1], __builtin_amdgcn_exp2f(v[i][0] - mc), l);
+                M = mn;
+            }
+#pragma unroll
+            for (int sh = 1; sh < kSub; sh <<= 1) {
+                const float mo = __shfl_xor(M, sh, 64), lo = __shfl_xor(l, sh, 64);
+                const float mn = fmaxf(M, mo), mc = mn == kNegInf ? 0.f : mn;
+                l = l * __builtin_amdgcn_exp2f(M - mc) + lo * __builtin_amdgcn_exp2f(mo - mc);
+                M = mn;
+            }
+            x.lse = M + __builtin_amdgcn_logf(l);
+        }
+        return x;
+    };
+    auto meta_put = [&](int step, const Meta &x) {
+        if (tid % kSub == 0) {
+            s_row[step % 3][tid / kSub] = x.row;
+            s_lse[step % 3][tid / kSub] = x.lse;
+            s_pos[step % 3][tid / kSub] = x.pos;
+        }
+    };
+    // rows of a step into buffer step % 2: 64 / kPc rows per load
+    auto stage = [&](int step) {
+        constexpr int kRowsPer = 64 / kPc, kLoads = R / kRowsPer / kScoreWaves;
+        const uint32_t dst = lds_addr_of(&s_q[step & 1][0]);
+#pragma unroll
+        for (int i = 0; i < kLoads; i++) {
+            const int ld = i * kScoreWaves + wave, row = ld * kRowsPer + lane / kPc;
+            lds_gather16(s_row[step % 3][row] + ((lane % kPc) ^ (row % kPc)) * 8, dst + ld * 1024);
+        }
+    };
+    float sum[2] = {0.f, 0.f};
+    if (steps > 0) {
+        meta_put(0, meta_load(0));
+        __syncthreads();
+        stage(0);
+        if (steps > 1)
+            meta_put(1, meta_load(1));
+        dma_wait_barrier();
+    }
+#pragma unroll 1
+    for (int step = 0; step < steps; step++) {
+        const uint16_t *q = &s_q[step & 1][0];
+        const float *lse = s_lse[step % 3];
+        const int *pos = s_pos[step % 3];
+        Meta next;
+        if (step + 1 < steps)
+            stage(step + 1);
+        if (step + 2 < steps)
+            next = meta_load(step + 2);
+        // scores of block x (of this wave's share of the step's rows)
+        auto scores = [&](int x, f32x16 (&s)[2]) {
+            const int row = (x * RW + rw) * 32 + m;
+            s[0] = f32x16{};
+            s[1] = f32x16{};
+#pragma unroll
+            for (int ss = 0; ss < D / 16; ss++) {
+                const bf16x8 qf =
+                    *(const bf16x8 *)&q[row * D + (((ss * 2 + g) ^ (m % kPc)) * 8)];
+#pragma unroll
+                for (int kb = 0; kb < 2; kb++)
+                    s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf, kf[kb][ss], s[kb], 0, 0, 0);
+            }
+        };
+        // their weights on this lane's two keys, added to each other before
+        // they are added to the sum
+        auto weights = [&](int x, const f32x16 (&s)[2], auto masked) {
+            float part[2] = {0.f, 0.f};
+#pragma unroll
+            for (int qd = 0; qd < 4; qd++) {
+                const int r = (x * RW + rw) * 32 + qd * 8 + g * 4;
+                const f32x4 ls = *(const f32x4 *)&lse[r];
+#pragma unroll
+                for (int kb = 0; kb < 2; kb++)
 #pragma unroll
                     for (int i = 0; i < 4; i++) {
-                        float w = __builtin_amdgcn_exp2f(fmaf(s[q * 4 + i], a.scale_log2, -ls[i]));
-                        if (masked && key > s_pos[rb * 32 + q * 8 + g * 4 + i])
-                            w = 0.f;
-                        part += w;
+                        float w = __builtin_amdgcn_exp2f(
+                            fmaf(s[kb][qd * 4 + i], a.scale_log2, -ls[i]));
+                        if constexpr (decltype(masked)::value)
+                            w = my0 + kb * 32 + m > pos[r + i] ? 0.f : w;
+                        part[kb] += w;
                     }
-                }
-                sum[kb] += part;
+            }
+            sum[0] += part[0];
+            sum[1] += part[1];
+        };
+        // rows ascend: the first one's position bounds what all see
+        if (uni(pos[0]) < my0 + 63 || (step + 1) * R > rows) {
+#pragma unroll 1
+            for (int x = 0; x < kBlocks; x++) {
+                f32x16 s[2];
+                scores(x, s);
+                weights(x, s, std::true_type{});
+            }
+        } else {
+            f32x16 s[2][2];
+            scores(0, s[0]);
+#pragma unroll
+            for (int x = 0; x < kBlocks; x++) {
+                if (x + 1 < kBlocks)
+                    scores(x + 1, s[(x + 1) & 1]);
+                weights(x, s[x & 1], std::false_type{});
             }
         }
+        if (step + 2 < steps)
+            meta_put(step + 2, next);
+        dma_wait_barrier();
     }
     // lane pairs, then the waves that share the keys
+    float *s_sum = (float *)&s_q[0][0];
 #pragma unroll
     for (int kb = 0; kb < 2; kb++) {
         sum[kb] = pair_sum(sum[kb]);
         if (g == 0)
-            s_sum[rw][kw * 64 + kb * 32 + m] = sum[kb];
+            s_sum[(rw * KW + kw) * 64 + kb * 32 + m] = sum[kb];
     }
     __syncthreads();
     for (int x = tid; x < KW * 64; x += kScoreThreads) {
         const int key = key0 + x;
         if (key >= T)
             continue;
-        float v = s_sum[0][x];
+        float v = s_sum[x];
 #pragma unroll
         for (int i = 1; i < RW; i++)
-            v += s_sum[i][x];
+            v += s_sum[i * KW * 64 + x];
         const int64_t at = (int64_t)kvh * a.n + base + key;
         a.score[at] = (a.score_in ? a.score_in[at] : 0.f) + v;
     }
@@ -485,14 +577,10 @@ __global__ __launch_bounds__(kScoreThreads) void step_weights_kernel(const StepS
 
 template <int D>
 hipError_t launch_score_d(const ScoreArgs &a, hipStream_t s) {
-    if (a.lse_out) {
+    if (a.lse_part) {
         hipLaunchKernelGGL((score_lse_kernel<D>), dim3(a.lse_items), dim3(kScoreThreads), 0, s, a);
         hipError_t e = hipGetLastError();
         if (e != hipSuccess)
-            return e;
-        const int64_t n = (int64_t)a.cap * a.hq;
-        hipLaunchKernelGGL(score_lse_join_kernel, dim3((n + 255) / 256), dim3(256), 0, s, a);
-        if ((e = hipGetLastError()) != hipSuccess)
             return e;
     }
     if (a.key_waves == 4)

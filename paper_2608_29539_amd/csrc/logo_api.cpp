@@ -423,7 +423,7 @@ PrefixPlan prefix_plan(const logo_problem *p, const logo_prefix *x, bool share) 
 struct ScorePlan {
     int key_waves, lse_kc, lse_chunks;
     long long items, lse_items;
-    size_t lse, lse_part, total;
+    size_t total;
 };
 
 // Keys per workgroup (64, 128 or 256): the most that still makes 512
@@ -436,16 +436,13 @@ ScorePlan score_plan(const logo_problem *p, int32_t cap) {
     d.items = (N / (64 * d.key_waves) + B) * H;
     const long long tiles = ((long long)cap * G) / kLseRows + B;
     const long long maxL = std::max(1, p->max_seqlen);
-    long long chunks = std::min((512 + tiles * H - 1) / (tiles * H), (maxL + 255) / 256);
+    long long chunks = std::min((1024 + tiles * H - 1) / (tiles * H), (maxL + 511) / 512);
     chunks = std::min(chunks, 64LL);
     const long long kc = ((maxL + chunks - 1) / chunks + 63) / 64 * 64;
     d.lse_kc = (int)std::min(kc, (1LL << 31) - 64);
     d.lse_chunks = (int)((maxL + d.lse_kc - 1) / d.lse_kc);
     d.lse_items = tiles * H * d.lse_chunks;
-    d.lse = 0;
-    d.lse_part = align_up(sizeof(float) * (size_t)cap * p->num_q_heads);
-    d.total = d.lse_part +
-              align_up(2 * sizeof(float) * (size_t)cap * p->num_q_heads * d.lse_chunks);
+    d.total = align_up(2 * sizeof(float) * (size_t)cap * p->num_q_heads * d.lse_chunks);
     return d;
 }
 
@@ -1843,7 +1840,7 @@ logo_status logo_cache_score(const logo_problem *p, const logo_bf16 *q, const lo
     if (N == 0)
         return LOGO_OK;
     const int32_t cap = cu_sel ? sel_capacity : N;
-    if ((long long)cap * p->num_q_heads >= (1LL << 31))
+    if ((long long)cap * p->num_q_heads >= (1LL << 31) - 1024)
         return LOGO_ERR_UNSUPPORTED;
     const ScorePlan d = score_plan(p, cap);
     if (d.items >= (1LL << 31) || d.lse_items >= (1LL << 31))
@@ -1859,9 +1856,7 @@ logo_status logo_cache_score(const logo_problem *p, const logo_bf16 *q, const lo
     a.cu_sel = cu_sel;
     a.lse = lse;
     if (!lse && cap > 0) {
-        a.lse_out = (float *)((char *)ws + d.lse);
-        a.lse_part = (float *)((char *)ws + d.lse_part);
-        a.lse = a.lse_out;
+        a.lse_part = (float *)ws;
     }
     a.score_in = score_in;
     a.score = score;

@@ -279,8 +279,8 @@ constexpr int kLseRows = 128;               // flattened (rank, head) rows per w
 struct ScoreArgs {
     const uint16_t *q, *k;
     const int32_t *cu, *sel_idx, *cu_sel;    // sel_idx, cu_sel NULL: every token is a row
-    const float *lse;                        // [Hq][cap]
-    float *lse_out, *lse_part;               // lse to be computed (lse = lse_out), or NULL
+    const float *lse;                        // [Hq][cap], or NULL:
+    float *lse_part;                         // (m, l) [lse_chunks][Hq][cap], to be computed
     const float *score_in;                   // [Hkv][n] or NULL (zeros)
     float *score;
     int64_t n;                               // tokens
