@@ -280,21 +280,31 @@ __global__ __launch_bounds__(kScoreThreads, 2) void score_kernel(const ScoreArgs
     // address and see nothing.
     constexpr int kSub = kScoreThreads / R;
     struct Meta {
-        const uint16_t *row;
+        int tok, head;
+        bool seen;
         float lse;
-        int pos;
     };
-    auto meta_load = [&](int step) {
+    // rank and head (of the G) of the row that meta_load takes next, one step
+    // of R rows at a time without a division
+    int next_flat = tid / kSub, next_rank = s0 + next_flat / G, next_head = next_flat % G;
+    const int step_ranks = R / G, step_heads = R % G;
+    auto meta_load = [&]() {
         Meta x;
-        const int flat = step * R + tid / kSub, f = min(flat, rows - 1);
-        const int rank = s0 + f / G, head = kvh * G + f % G;
-        const int tok = token_of(a, rank);
-        x.pos = flat < rows ? tok - base : -1;
-        x.row = a.q + ((int64_t)tok * a.hq + head) * D;
+        const int rank = min(next_rank, s1 - 1), head = kvh * G + next_head;
+        x.tok = token_of(a, rank);
+        x.head = head;
+        x.seen = next_flat < rows;
+        next_flat += R;
+        next_rank += step_ranks;
+        next_head += step_heads;
+        if (next_head >= G) {
+            next_head -= G;
+            next_rank++;
+        }
         if (!a.lse_part) {
-            x.lse = a.lse[(int64_t)head * a.cap + rank];
+            x.lse = a.lse[head * a.cap + rank];
         } else {
-            const int n = min((tok - base) / a.lse_kc + 1, a.lse_chunks);
+            const int n = min((x.tok - base) / a.lse_kc + 1, a.lse_chunks);
             const f32x2 *pp = (const f32x2 *)a.lse_part + (int64_t)head * a.cap + rank;
             const int64_t stride = (int64_t)a.hq * a.cap;
             float M = kNegInf, l = 0.f;
@@ -323,11 +333,14 @@ __global__ __launch_bounds__(kScoreThreads, 2) void score_kernel(const ScoreArgs
         }
         return x;
     };
-    auto meta_put = [&](int step, const Meta &x) {
+    auto meta_put = [&](int step, Meta x) {
+        // not before here: a wait for these loads at the step's start would
+        // wait for the rows that are loaded behind them too
+        asm volatile("" : "+v"(x.tok), "+v"(x.lse));
         if (tid % kSub == 0) {
-            s_row[step % 3][tid / kSub] = x.row;
+            s_row[step % 3][tid / kSub] = a.q + ((int64_t)x.tok * a.hq + x.head) * D;
             s_lse[step % 3][tid / kSub] = x.lse;
-            s_pos[step % 3][tid / kSub] = x.pos;
+            s_pos[step % 3][tid / kSub] = x.seen ? x.tok - base : -1;
         }
     };
     // rows of a step into buffer step % 2: 64 / kPc rows per load
@@ -342,11 +355,11 @@ __global__ __launch_bounds__(kScoreThreads, 2) void score_kernel(const ScoreArgs
     };
     float sum[2] = {0.f, 0.f};
     if (steps > 0) {
-        meta_put(0, meta_load(0));
+        meta_put(0, meta_load());
         __syncthreads();
         stage(0);
         if (steps > 1)
-            meta_put(1, meta_load(1));
+            meta_put(1, meta_load());
         dma_wait_barrier();
     }
 #pragma unroll 1
@@ -354,11 +367,11 @@ __global__ __launch_bounds__(kScoreThreads, 2) void score_kernel(const ScoreArgs
         const uint16_t *q = &s_q[step & 1][0];
         const float *lse = s_lse[step % 3];
         const int *pos = s_pos[step % 3];
-        Meta next;
+        Meta next = {};
+        if (step + 2 < steps)
+            next = meta_load();
         if (step + 1 < steps)
             stage(step + 1);
-        if (step + 2 < steps)
-            next = meta_load(step + 2);
         // scores of block x (of this wave's share of the step's rows)
         auto scores = [&](int x, f32x16 (&s)[2]) {
             const int row = (x * RW + rw) * 32 + m;
