@@ -454,12 +454,37 @@ __global__ __launch_bounds__(kScoreThreads, 2) void score_kernel(const ScoreArgs
 
 // ---------------------------------------------------------------------------
 // One decoding step.  The scores of a chunk of keys: 16 x 16 x 32 products of
-// up to 16 heads (rows, of which G exist) and 16 keys; lane l holds key l % 16
-// and heads 4 (l / 16) + 0..3.
+// the heads (rows) and 16 keys (columns).  With 4 P heads (P = 1, 2 or 4, heads
+// past the last repeat it) the rows hold them 4 / P times, so that lane l's
+// four rows are heads 4 ((l / 16) % P) + 0..3 whichever copy it looks at; of
+// the four products of 64 keys it keeps those P whose keys are its own, and
+// every lane has P keys' scores of four heads to exponentiate and store in
+// whole lines.
+//
+// Bound by reading K.  Each wave streams keys of its own, 16 at a time, through
+// a ring of slots in LDS (32 KB) filled by direct loads, whose lanes read
+// whole rows (a row's 16-byte pieces permuted as in score_kernel); no barrier,
+// a wave waits for its own oldest slots.  Workgroups of two waves, so that two
+// of them share a CU's LDS and one's start and end hide behind the other.
 // ---------------------------------------------------------------------------
+constexpr int kStepWaves = 2;
 template <int D>
-__global__ __launch_bounds__(kScoreThreads) void step_logits_kernel(const StepScoreArgs a) {
-    __shared__ f32x2 s_ml[kScoreWaves][16];
+constexpr int step_ring() { return D == 128 ? 8 : 16; }
+
+// Waits until at most N of the wave's vector-memory operations are outstanding.
+template <int N>
+__device__ __forceinline__ void wait_outstanding() {
+    constexpr int n = N < 63 ? N : 63;
+    __builtin_amdgcn_s_waitcnt(kWaitVmcnt0 | (n & 15) | ((n >> 4) << 14));
+}
+
+template <int D, int P>
+__global__ __launch_bounds__(kStepWaves * 64) void step_logits_kernel(const StepScoreArgs a) {
+    constexpr int kRing = step_ring<D>(), kPc = D / 8;
+    constexpr int kLoads = 16 * D * 2 / 1024;              // loads per slot
+    constexpr int kCopies = 4 / P;
+    __shared__ __attribute__((aligned(16))) uint16_t s_k[kStepWaves][kRing][16 * D];
+    __shared__ f32x2 s_ml[kStepWaves][16];
     const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6);
     const int kg = lane >> 4, n = lane & 15;
     const int G = a.group;
@@ -471,63 +496,119 @@ __global__ __launch_bounds__(kScoreThreads) void step_logits_kernel(const StepSc
     const int c = item % a.chunks, b = item / a.chunks;
     if (!(a.gate[b] > decode_threshold(a)))
         return;
-    const int64_t base = a.cu[b];
-    const int L = a.cu[b + 1] - (int)base;
+    const int base = a.cu[b];
+    const int L = a.cu[b + 1] - base;
     const int k0 = c * a.kc, k1 = min(L, k0 + a.kc);
     if (k0 >= k1)
         return;
-    const int nh = min(16, G - hb * 16), h0 = kvh * G + hb * 16;
+    // this wave's keys: its share of the chunk's blocks of 64
+    const int blocks = (k1 - k0 + 63) / 64, per = (blocks + kStepWaves - 1) / kStepWaves;
+    const int w0 = k0 + wave * per * 64, w1 = min(k1, w0 + per * 64);
+    const uint16_t *kb = a.k + ((int64_t)base * a.hkv + kvh) * D;
+    const int64_t stride = (int64_t)a.hkv * D;
+    // slot i of the wave: keys w0 + 16 i .. + 15; past the last key its row again
+    const int slots = w1 > w0 ? ((w1 - w0 + 63) / 64) * 4 : 0;
+    auto stage = [&](int i) {
+        const uint32_t dst = lds_addr_of(&s_k[wave][i % kRing][0]);
+#pragma unroll
+        for (int x = 0; x < kLoads; x++) {
+            const int row = x * (16 / kLoads) + lane / kPc;
+            const int key = min(w0 + i * 16 + row, w1 - 1);
+            lds_gather16(kb + key * stride + ((lane % kPc) ^ (row % kPc)) * 8, dst + x * 1024);
+        }
+    };
+    const int nh = min(4 * P, G - hb * 4 * P), h0 = kvh * G + hb * 4 * P;
     bf16x8 qf[D / 32];
+    {
+        const int h = h0 + min(n % (4 * P), nh - 1);
+#pragma unroll
+        for (int s = 0; s < D / 32; s++)
+            qf[s] = *(const bf16x8 *)(a.q + ((int64_t)b * a.hq + h) * D + s * 32 + kg * 8);
+    }
+    // (waited for before the ring is filled: a wait inside the loop would be
+    // for the ring too)
 #pragma unroll
     for (int s = 0; s < D / 32; s++)
-        qf[s] = n < nh ? *(const bf16x8 *)(a.q + ((int64_t)b * a.hq + h0 + n) * D + s * 32 + kg * 8)
-                       : bf16x8{};
+        asm volatile("" : "+v"(qf[s]));
+    for (int i = 0; i < min(kRing, slots); i++)
+        stage(i);
     float mr[4], l[4];
 #pragma unroll
     for (int i = 0; i < 4; i++) {
         mr[i] = kNegInf;
         l[i] = 0.f;
     }
-    const uint16_t *kb = a.k + (base * a.hkv + kvh) * (int64_t)D + kg * 8;
-    for (int key = k0 + wave * 16; key < k1; key += kScoreWaves * 16) {
-        const int j = key + n;
-        const uint16_t *kp = kb + (int64_t)j * a.hkv * D;
-        f32x4 s = {};
+    for (int s0 = 0; s0 < slots; s0 += 4) {
+        f32x4 own[P];
+        // The four slots are in when no more than what was issued behind them
+        // is outstanding: the loads of the ring's other slots, and the stores
+        // of the last kRing / 4 steps where there were as many.
+        constexpr int kBehind = (kRing - 4) * kLoads;
+        if (s0 + kRing > slots)
+            wait_outstanding<0>();
+        else if (s0 < kRing)
+            wait_outstanding<kBehind>();
+        else
+            wait_outstanding<kBehind + kRing * P>();
+        asm volatile("" ::: "memory");
 #pragma unroll
-        for (int x = 0; x < D / 32; x++) {
-            const bf16x8 kf = j < k1 ? *(const bf16x8 *)(kp + x * 32) : bf16x8{};
-            s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[x], kf, s, 0, 0, 0);
+        for (int j = 0; j < 4; j++) {
+            const uint16_t *t = &s_k[wave][(s0 + j) % kRing][0];
+            f32x4 s = {};
+#pragma unroll
+            for (int x = 0; x < D / 32; x++) {
+                const bf16x8 kf =
+                    *(const bf16x8 *)&t[n * D + (((x * 4 + kg) ^ (n % kPc)) * 8)];
+                s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[x], kf, s, 0, 0, 0);
+            }
+            // keys 16 j .. + 15 belong to copy j % kCopies
+            if (kCopies == 1 || kg / P == j % kCopies)
+                own[j / kCopies] = s;
+        }
+        asm volatile("" ::: "memory");
+        if (s0 + kRing < slots) {
+            // (the fragments have been read: the products took them)
+#pragma unroll
+            for (int j = 0; j < 4; j++)
+                stage(s0 + kRing + j);
         }
 #pragma unroll
-        for (int i = 0; i < 4; i++) {
-            const int h = kg * 4 + i;
-            const float v = s[i] * a.scale_log2;
-            if (h < nh && j < k1)
-                a.logits[(int64_t)(h0 + h) * a.n + base + j] = v;
-            const float x = j < k1 ? v : kNegInf;
-            const float mn = fmaxf(mr[i], x), mc = mn == kNegInf ? 0.f : mn;
-            l[i] = fmaf(l[i], __builtin_amdgcn_exp2f(mr[i] - mc), __builtin_amdgcn_exp2f(x - mc));
-            mr[i] = mn;
+        for (int x = 0; x < P; x++) {
+            const int key = w0 + s0 * 16 + (x * kCopies + kg / P) * 16 + n;
+            // (the lanes past the last key or head have its score and store
+            // it again: the number of stores is what the waits count on)
+            float *lp = a.logits + base + min(key, w1 - 1);
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                const float v = own[x][i] * a.scale_log2;
+                lp[(int64_t)(h0 + min(4 * (kg % P) + i, nh - 1)) * a.n] = v;
+                const float y = key < w1 ? v : kNegInf;
+                const float mn = fmaxf(mr[i], y), mc = mn == kNegInf ? 0.f : mn;
+                l[i] = fmaf(l[i], __builtin_amdgcn_exp2f(mr[i] - mc), __builtin_amdgcn_exp2f(y - mc));
+                mr[i] = mn;
+            }
         }
     }
-    // the 16 lanes of a head, then the waves
+    // the lanes of a head (all but the bits of (kg % P)), then the waves
 #pragma unroll
     for (int i = 0; i < 4; i++) {
 #pragma unroll
-        for (int sh = 1; sh < 16; sh <<= 1) {
+        for (int sh = 1; sh < 64; sh <<= 1) {
+            if (sh >= 16 && sh < 16 * P)
+                continue;
             const float mo = __shfl_xor(mr[i], sh, 64), lo = __shfl_xor(l[i], sh, 64);
             const float mn = fmaxf(mr[i], mo), mc = mn == kNegInf ? 0.f : mn;
             l[i] = l[i] * __builtin_amdgcn_exp2f(mr[i] - mc) + lo * __builtin_amdgcn_exp2f(mo - mc);
             mr[i] = mn;
         }
-        if (n == 0)
+        if (n == 0 && kg < P)
             s_ml[wave][kg * 4 + i] = f32x2{mr[i], l[i]};
     }
     __syncthreads();
     if (tid < nh) {
         float M = kNegInf, sum = 0.f;
 #pragma unroll
-        for (int w = 0; w < kScoreWaves; w++) {
+        for (int w = 0; w < kStepWaves; w++) {
             const f32x2 v = s_ml[w][tid];
             const float mn = fmaxf(M, v[0]), mc = mn == kNegInf ? 0.f : mn;
             sum = sum * __builtin_amdgcn_exp2f(M - mc) + v[1] * __builtin_amdgcn_exp2f(v[0] - mc);
@@ -612,15 +693,27 @@ hipError_t launch_cache_score(const ScoreArgs &a, hipStream_t s) {
 }
 
 hipError_t launch_decode_score(const StepScoreArgs &a, hipStream_t s) {
-    const dim3 grid(a.items), block(kScoreThreads);
+    auto launch = [&](auto d, auto p) {
+        hipLaunchKernelGGL((step_logits_kernel<decltype(d)::value, decltype(p)::value>),
+                           dim3(a.items), dim3(kStepWaves * 64), 0, s, a);
+    };
+    auto launch_d = [&](auto d) {
+        if (a.head_copies == 4)
+            launch(d, std::integral_constant<int, 1>{});
+        else if (a.head_copies == 2)
+            launch(d, std::integral_constant<int, 2>{});
+        else
+            launch(d, std::integral_constant<int, 4>{});
+    };
     if (a.head_dim == 128)
-        hipLaunchKernelGGL((step_logits_kernel<128>), grid, block, 0, s, a);
+        launch_d(std::integral_constant<int, 128>{});
     else
-        hipLaunchKernelGGL((step_logits_kernel<64>), grid, block, 0, s, a);
+        launch_d(std::integral_constant<int, 64>{});
     hipError_t e = hipGetLastError();
     if (e != hipSuccess)
         return e;
-    hipLaunchKernelGGL(step_weights_kernel, dim3(a.out_items), block, a.group * sizeof(float), s, a);
+    hipLaunchKernelGGL(step_weights_kernel, dim3(a.out_items), dim3(kScoreThreads),
+                       a.group * sizeof(float), s, a);
     return hipGetLastError();
 }
 

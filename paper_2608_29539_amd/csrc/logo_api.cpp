@@ -426,13 +426,16 @@ struct ScorePlan {
     size_t total;
 };
 
-// Keys per workgroup (64, 128 or 256): the most that still makes 512
-// workgroups, two per CU.  Key chunks of the log-sum-exp likewise, of at least 256 keys.
+// Keys per workgroup (64, 128 or 256): the most that still makes 256
+// workgroups, one per CU.  More keys share the staged rows; fewer make up for
+// a small problem: 64 rows on 13324 keys, 8 KV heads, 21.8 us with 256 keys,
+// 29.5 with 128, 47.8 with 64; 256 rows on 1024 keys, 2 KV heads, d = 64, 29.3,
+// 20.4 and 14.7.  Key chunks of the log-sum-exp: about 1024 workgroups, of at least 512 keys.
 ScorePlan score_plan(const logo_problem *p, int32_t cap) {
     ScorePlan d;
     const long long N = p->total_tokens, B = p->num_seqs, H = p->num_kv_heads;
     const long long G = p->num_q_heads / p->num_kv_heads;
-    d.key_waves = N * H >= 512 * 256 ? 4 : N * H >= 512 * 128 ? 2 : 1;
+    d.key_waves = N * H >= 256 * 256 ? 4 : N * H >= 256 * 128 ? 2 : 1;
     d.items = (N / (64 * d.key_waves) + B) * H;
     const long long tiles = ((long long)cap * G) / kLseRows + B;
     const long long maxL = std::max(1, p->max_seqlen);
@@ -447,7 +450,7 @@ ScorePlan score_plan(const logo_problem *p, int32_t cap) {
 }
 
 struct StepScorePlan {
-    int kc, chunks, out_chunks, head_blocks;
+    int kc, chunks, out_chunks, head_copies, head_blocks;
     long long items, out_items;
     size_t ml, total;
 };
@@ -455,8 +458,11 @@ StepScorePlan step_score_plan(const logo_problem *p) {
     StepScorePlan d;
     const long long maxL = std::max(1, p->max_seqlen), B = p->num_seqs, H = p->num_kv_heads;
     const long long G = p->num_q_heads / p->num_kv_heads;
+    d.head_copies = G <= 4 ? 4 : G <= 8 ? 2 : 1;
     d.head_blocks = (int)((G + 15) / 16);
-    d.kc = 512;
+    d.kc = 2048;
+    while (d.kc > 256 && B * H * d.head_blocks * ((maxL + d.kc - 1) / d.kc) < 512)
+        d.kc /= 2;
     d.chunks = (int)((maxL + d.kc - 1) / d.kc);
     d.out_chunks = (int)((maxL + kStepKeys - 1) / kStepKeys);
     d.items = B * H * d.head_blocks * d.chunks;
@@ -1920,6 +1926,7 @@ logo_status logo_decode_score(const logo_problem *p, const logo_bf16 *q, const l
     a.hkv = p->num_kv_heads;
     a.group = p->num_q_heads / p->num_kv_heads;
     a.head_dim = p->head_dim;
+    a.head_copies = d.head_copies;
     a.head_blocks = d.head_blocks;
     a.scale_log2 = scale_log2(p);
     a.kc = d.kc;

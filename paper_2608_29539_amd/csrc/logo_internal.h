@@ -299,7 +299,8 @@ struct StepScoreArgs {
     const float *score_in;                   // [Hkv][n] or NULL (zeros)
     float *score, *logits, *ml;              // logits [Hq][n]; ml [B][Hq][chunks][2]
     int64_t n;
-    int32_t num_seqs, hq, hkv, group, head_dim, head_blocks;
+    int32_t num_seqs, hq, hkv, group, head_dim;
+    int32_t head_copies, head_blocks;        // 16 rows hold 16 / head_copies heads, head_copies times
     float scale_log2;
     int32_t kc, chunks, items, out_chunks, out_items;
     int32_t sel_mode;                        // as PrefixArgs
