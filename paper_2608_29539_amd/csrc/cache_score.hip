@@ -489,11 +489,11 @@ __global__ __launch_bounds__(kStepWaves * 64) void step_logits_kernel(const Step
     const int kg = lane >> 4, n = lane & 15;
     const int G = a.group;
     int item = blockIdx.x;
-    const int kvh = item % a.hkv;
-    item /= a.hkv;
+    const int c = item % a.chunks;
+    item /= a.chunks;
     const int hb = item % a.head_blocks;
     item /= a.head_blocks;
-    const int c = item % a.chunks, b = item / a.chunks;
+    const int kvh = item % a.hkv, b = item / a.hkv;
     if (!(a.gate[b] > decode_threshold(a)))
         return;
     const int base = a.cu[b];
@@ -661,12 +661,27 @@ __global__ __launch_bounds__(kScoreThreads) void step_weights_kernel(const StepS
             s_lse[h] = M + __builtin_amdgcn_logf(l);
     }
     __syncthreads();
-    for (int j = k0 + tid; j < k1; j += kScoreThreads) {
-        float w = 0.f;
-        for (int h = 0; h < G; h++)
-            w += __builtin_amdgcn_exp2f(a.logits[(int64_t)(kvh * G + h) * a.n + base + j] - s_lse[h]);
-        a.score[at + j] = (a.score_in ? a.score_in[at + j] : 0.f) + w;
+    // every key's scores are on their way before the first sum is stored
+    constexpr int kPer = kStepKeys / kScoreThreads;
+    float w[kPer], in[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; i++) {
+        const int j = min(k0 + tid + i * kScoreThreads, k1 - 1);
+        in[i] = a.score_in ? a.score_in[at + j] : 0.f;
+        w[i] = 0.f;
     }
+#pragma unroll 4
+    for (int h = 0; h < G; h++) {
+        const float *lp = a.logits + (int64_t)(kvh * G + h) * a.n + base;
+        const float lse = s_lse[h];
+#pragma unroll
+        for (int i = 0; i < kPer; i++)
+            w[i] += __builtin_amdgcn_exp2f(lp[min(k0 + tid + i * kScoreThreads, k1 - 1)] - lse);
+    }
+#pragma unroll
+    for (int i = 0; i < kPer; i++)
+        if (k0 + tid + i * kScoreThreads < k1)
+            a.score[at + k0 + tid + i * kScoreThreads] = in[i] + w[i];
 }
 
 template <int D>

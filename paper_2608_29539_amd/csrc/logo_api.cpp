@@ -449,6 +449,9 @@ ScorePlan score_plan(const logo_problem *p, int32_t cap) {
     return d;
 }
 
+// Keys per chunk of the scores' pass: 1024, down to 256 while there are fewer
+// than 512 workgroups (two per CU).  16 caches of 32K tokens, 8 KV heads: 256
+// keys 254 us, 512 and 1024 220, 2048 229, 4096 258.
 struct StepScorePlan {
     int kc, chunks, out_chunks, head_copies, head_blocks;
     long long items, out_items;
@@ -460,7 +463,7 @@ StepScorePlan step_score_plan(const logo_problem *p) {
     const long long G = p->num_q_heads / p->num_kv_heads;
     d.head_copies = G <= 4 ? 4 : G <= 8 ? 2 : 1;
     d.head_blocks = (int)((G + 15) / 16);
-    d.kc = 2048;
+    d.kc = 1024;
     while (d.kc > 256 && B * H * d.head_blocks * ((maxL + d.kc - 1) / d.kc) < 512)
         d.kc /= 2;
     d.chunks = (int)((maxL + d.kc - 1) / d.kc);
