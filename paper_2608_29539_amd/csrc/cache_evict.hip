@@ -5,11 +5,17 @@
 // others the k with the largest scores (a NaN is the lowest, -0 equals +0, ties
 // go to the lowest index), in ascending order.
 //
-//   evict_select_kernel  one workgroup per (sequence, KV head): the k-th
-//                        largest score by radix selection on order-preserving
-//                        32-bit keys (histograms of 11, 11 and 10 bits in LDS),
-//                        then one pass that ranks the rows above it and the
-//                        first ones equal to it
+// The k-th largest is found by radix selection on order-preserving 32-bit keys
+// (11, 11 and 10 bits), and the rows above it and the first ones equal to it
+// get their places by counting.  A workgroup has 8192 rows in registers.
+//
+//   evict_select_kernel  caches of up to 8192 rows: one workgroup per (sequence,
+//                        KV head) does it all, with the histograms in LDS
+//   evict_hist_kernel    longer ones: a launch per digit, in which every part
+//                        of 8192 rows adds up all parts' last histograms, picks
+//                        the bin of the k-th and counts the next digit
+//   evict_rank_kernel    picks the last digit and places its part's rows, the
+//                        counts of the parts before it added up
 //   evict_copy_kernel    copies the kept rows of K and V
 #include "attn_common.h"
 #include "logo_internal.h"
@@ -19,6 +25,7 @@ namespace {
 
 constexpr int kEvThreads = 1024;
 constexpr int kEvWaves = kEvThreads / 64;
+constexpr int kEvPer = kEvPartRows / kEvThreads;           // rows per thread
 constexpr int kEvBins = 2048;
 
 // Order-preserving key of a score: a larger score has a larger key, NaN 0.
@@ -54,88 +61,260 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t *s_part, uin
     return before + incl - v;
 }
 
+// One (sequence, KV head): n rows stay of L, k of the first `old` by score.
+struct Choice {
+    int b, h, base, L, n, rec, k, old;
+    const float *score;
+    __device__ __forceinline__ Choice(const EvictArgs &a, int problem) {
+        b = problem / a.hkv;
+        h = problem % a.hkv;
+        base = a.cu[b];
+        L = a.cu[b + 1] - base;
+        n = min(L, a.budget);
+        rec = min(a.recent, n);
+        k = n - rec;
+        old = L - rec;
+        score = a.score + (int64_t)h * a.n + base;
+    }
+    __device__ __forceinline__ bool by_score() const { return k > 0 && k < old; }
+};
+
+// A part's rows in registers, each wave 512 consecutive ones: row
+// part * kEvPartRows + wave * 512 + j * 64 + lane.
+struct Rows {
+    float x[kEvPer];
+    int first, old;
+    __device__ __forceinline__ int row(int j) const { return first + j * 64; }
+    __device__ __forceinline__ bool in(int j) const { return row(j) < old; }
+    __device__ __forceinline__ Rows(const Choice &c, int part) {
+        first = part * kEvPartRows + (threadIdx.x >> 6) * (64 * kEvPer) + (threadIdx.x & 63);
+        old = c.old;
+#pragma unroll
+        for (int j = 0; j < kEvPer; j++)
+            x[j] = in(j) ? c.score[row(j)] : 0.f;
+    }
+};
+
+// The digits found so far: keys that agree with `prefix` under `mask`, `left`
+// of them (the largest) stay.
+struct Digits {
+    uint32_t prefix = 0, mask = 0, left = 0;
+    __device__ __forceinline__ static int shift(int level) { return level == 0 ? 21 : level == 1 ? 10 : 0; }
+    __device__ __forceinline__ static uint32_t width(int level) { return level == 2 ? 1023 : 2047; }
+    __device__ __forceinline__ void take(int level, uint32_t bin, uint32_t in_bin) {
+        prefix |= bin << shift(level);
+        mask |= width(level) << shift(level);
+        left = in_bin;
+    }
+};
+
+// Histogram of digit `level` of the rows that agree with the digits so far.
+__device__ __forceinline__ void count_digit(const Rows &r, const Digits &d, int level,
+                                            uint32_t *s_hist) {
+    for (int i = threadIdx.x; i < kEvBins; i += kEvThreads)
+        s_hist[i] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kEvPer; j++) {
+        const uint32_t key = score_key(r.x[j]);
+        if (r.in(j) && (key & d.mask) == d.prefix)
+            atomicAdd(&s_hist[(key >> Digits::shift(level)) & Digits::width(level)], 1u);
+    }
+    __syncthreads();
+}
+
+// The bin in which the `left`-th largest lies, from this thread's bins 2047 -
+// 2 tid (c0) and 2046 - 2 tid (c1); s_pick: the bin and how many of it stay.
+__device__ __forceinline__ void pick_bin(uint32_t c0, uint32_t c1, uint32_t left, uint32_t *s_part,
+                                         uint32_t *s_pick) {
+    uint32_t total;
+    const uint32_t above = block_scan(c0 + c1, s_part, total);
+    if (above < left && left <= above + c0 + c1) {
+        const bool first = left <= above + c0;
+        s_pick[0] = kEvBins - 1 - 2 * threadIdx.x - (first ? 0 : 1);
+        s_pick[1] = left - above - (first ? 0 : c0);
+    }
+    __syncthreads();
+}
+
+// Places of a part's rows: all of them, or those above the pivot and the
+// first `need` equal to it; gt0, eq0: such rows before the part.
+__device__ __forceinline__ void place(const EvictArgs &a, const Choice &c, const Rows &r, bool all,
+                                      uint32_t pivot, uint32_t need, uint32_t gt0, uint32_t eq0,
+                                      uint32_t off, uint32_t *s_part) {
+    const int lane = threadIdx.x & 63;
+    const uint64_t below = (1ull << lane) - 1;
+    uint32_t gt = 0, eq = 0;                               // of this wave
+#pragma unroll
+    for (int j = 0; j < kEvPer; j++) {
+        const uint32_t key = score_key(r.x[j]);
+        gt += (uint32_t)__popcll(__ballot(r.in(j) && (all || key > pivot)));
+        eq += (uint32_t)__popcll(__ballot(r.in(j) && !all && key == pivot));
+    }
+    uint32_t total;
+    const uint32_t ex = block_scan(lane == 0 ? gt | eq << 16 : 0u, s_part, total);
+    gt0 += __shfl(ex, 0, 64) & 0xFFFFu;
+    eq0 += __shfl(ex, 0, 64) >> 16;
+    const int64_t out = (int64_t)c.h * a.cap + off;
+    const int room = a.cap - (int)off;                     // (n, for a capacity as documented)
+#pragma unroll
+    for (int j = 0; j < kEvPer; j++) {
+        const uint32_t key = score_key(r.x[j]);
+        const bool g = r.in(j) && (all || key > pivot), e = r.in(j) && !all && key == pivot;
+        const uint64_t gm = __ballot(g), em = __ballot(e);
+        const uint32_t eb = eq0 + (uint32_t)__popcll(em & below);
+        const uint32_t at = gt0 + (uint32_t)__popcll(gm & below) + min(eb, need);
+        if ((g || (e && eb < need)) && (int)at < room) {
+            a.keep_idx[out + at] = c.base + r.row(j);
+            a.score_out[out + at] = r.x[j];
+        }
+        gt0 += (uint32_t)__popcll(gm);
+        eq0 += (uint32_t)__popcll(em);
+    }
+}
+
+// Rows that the sequences before this one keep; cu_keep; the newest rows, of
+// which workgroup `part` of `parts` places its share.
+__device__ __forceinline__ uint32_t place_recent(const EvictArgs &a, const Choice &c, int part,
+                                                 int parts, uint32_t *s_part) {
+    const int tid = threadIdx.x;
+    uint32_t mine = 0, off;
+    for (int i = tid; i < c.b; i += kEvThreads)
+        mine += min(a.cu[i + 1] - a.cu[i], a.budget);
+    block_scan(mine, s_part, off);
+    if (c.h == 0 && part == 0 && tid == 0) {
+        if (c.b == 0)
+            a.cu_keep[0] = 0;
+        a.cu_keep[c.b + 1] = (int)off + c.n;
+    }
+    const int64_t out = (int64_t)c.h * a.cap + off + c.k;
+    const int room = a.cap - (int)off - c.k;
+    for (int i = part * kEvThreads + tid; i < min(c.rec, room); i += parts * kEvThreads) {
+        a.keep_idx[out + i] = c.base + c.old + i;
+        a.score_out[out + i] = c.score[c.old + i];
+    }
+    return off;
+}
+
 __global__ __launch_bounds__(kEvThreads) void evict_select_kernel(const EvictArgs a) {
     __shared__ uint32_t s_hist[kEvBins], s_part[kEvWaves], s_pick[2];
     const int tid = threadIdx.x;
-    const int b = blockIdx.x / a.hkv, h = blockIdx.x % a.hkv;
-    // rows that the sequences before this one keep
-    uint32_t off = 0;
-    {
-        uint32_t mine = 0;
-        for (int i = tid; i < b; i += kEvThreads)
-            mine += min(a.cu[i + 1] - a.cu[i], a.budget);
-        block_scan(mine, s_part, off);
+    const Choice c(a, blockIdx.x);
+    const Rows r(c, 0);
+    const uint32_t off = place_recent(a, c, 0, 1, s_part);
+    Digits d;
+    d.left = c.k;
+    if (c.by_score()) {
+#pragma unroll 1
+        for (int level = 0; level < 3; level++) {
+            count_digit(r, d, level, s_hist);
+            pick_bin(s_hist[kEvBins - 1 - 2 * tid], s_hist[kEvBins - 2 - 2 * tid], d.left, s_part,
+                     s_pick);
+            d.take(level, s_pick[0], s_pick[1]);
+        }
     }
-    const int64_t base = a.cu[b];
-    const int L = a.cu[b + 1] - (int)base;
-    const int n = min(L, a.budget), rec = min(a.recent, n), k = n - rec, old = L - rec;
-    if (h == 0 && tid == 0) {
-        if (b == 0)
-            a.cu_keep[0] = 0;
-        a.cu_keep[b + 1] = (int)off + n;
-    }
-    const float *sc = a.score + (int64_t)h * a.n + base;
-    const int64_t out = (int64_t)h * a.cap + off;
-    const int room = a.cap - (int)off;                     // (n, for a capacity as documented)
+    if (c.k > 0)
+        place(a, c, r, c.k == c.old, d.prefix, d.left, 0, 0, off, s_part);
+}
 
-    uint32_t pivot = 0, need = 0;                          // the k-th key, rows equal to it kept
-    if (k > 0 && k < old) {
-        uint32_t prefix = 0, mask = 0, left = k;
-        for (int pass = 0; pass < 3; pass++) {
-            const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
-            const uint32_t width = pass == 2 ? 1023 : 2047;
-            for (int i = tid; i < kEvBins; i += kEvThreads)
-                s_hist[i] = 0;
-            __syncthreads();
-            for (int i = tid; i < old; i += kEvThreads) {
-                const uint32_t key = score_key(sc[i]);
-                if ((key & mask) == prefix)
-                    atomicAdd(&s_hist[(key >> shift) & width], 1u);
-            }
-            __syncthreads();
-            // bins from the largest: this thread's two
-            const uint32_t c0 = s_hist[kEvBins - 1 - 2 * tid], c1 = s_hist[kEvBins - 2 - 2 * tid];
-            uint32_t total;
-            const uint32_t above = block_scan(c0 + c1, s_part, total);
-            if (above < left && left <= above + c0 + c1) {
-                const bool first = left <= above + c0;
-                s_pick[0] = kEvBins - 1 - 2 * tid - (first ? 0 : 1);
-                s_pick[1] = left - above - (first ? 0 : c0);
-            }
-            __syncthreads();
-            prefix |= s_pick[0] << shift;
-            mask |= width << shift;
-            left = s_pick[1];
-            __syncthreads();
-        }
-        pivot = prefix;
-        need = left;
-    }
-    if (k > 0) {
-        const bool all = k == old;
-        uint32_t gt0 = 0, eq0 = 0;                         // rows before this step
-        for (int i0 = 0; i0 < old; i0 += kEvThreads) {
-            const int i = i0 + tid;
-            const float x = i < old ? sc[i] : 0.f;
-            const uint32_t key = score_key(x);
-            const bool gt = i < old && (all || key > pivot), eq = i < old && !all && key == pivot;
-            uint32_t total;
-            const uint32_t ex = block_scan((gt ? 1u : 0u) | (eq ? 0x10000u : 0u), s_part, total);
-            const uint32_t gb = gt0 + (ex & 0xFFFFu), eb = eq0 + (ex >> 16);
-            const uint32_t at = gb + min(eb, need);
-            if ((gt || (eq && eb < need)) && (int)at < room) {
-                a.keep_idx[out + at] = (int)base + i;
-                a.score_out[out + at] = x;
-            }
-            gt0 += total & 0xFFFFu;
-            eq0 += total >> 16;
+// Two 16-bit bins per word: word 1023 - t holds thread t's bins.
+__device__ __forceinline__ uint32_t *hist_of(const EvictArgs &a, int level, int problem, int part) {
+    return a.hist + (((int64_t)(level & 1) * a.num_seqs * a.hkv + problem) * a.parts + part) *
+                        (kEvBins / 2);
+}
+// This thread's bins over all parts with rows by score, and over those before
+// `part`.
+struct Bins {
+    uint32_t c0 = 0, c1 = 0, before0 = 0, before1 = 0;
+    __device__ __forceinline__ Bins(const EvictArgs &a, const Choice &c, int level, int problem,
+                                    int part) {
+        const int n = (c.old + kEvPartRows - 1) / kEvPartRows;
+        const uint32_t *w = hist_of(a, level, problem, 0) + (kEvBins / 2 - 1 - threadIdx.x);
+#pragma unroll 8
+        for (int i = 0; i < n; i++) {
+            const uint32_t v = w[(int64_t)i * (kEvBins / 2)];
+            c0 += v >> 16;
+            c1 += v & 0xFFFFu;
+            before0 += i < part ? v >> 16 : 0u;
+            before1 += i < part ? v & 0xFFFFu : 0u;
         }
     }
-    for (int i = tid; i < rec; i += kEvThreads)
-        if (k + i < room) {
-            a.keep_idx[out + k + i] = (int)base + old + i;
-            a.score_out[out + k + i] = sc[old + i];
+};
+
+// LEVEL 0, 1, 2: the digits before it are picked (the last from the
+// histograms, an earlier one as part 0 of its launch wrote it), the part's
+// rows above the last pick are counted, and its digit LEVEL.
+template <int LEVEL>
+__global__ __launch_bounds__(kEvThreads) void evict_hist_kernel(const EvictArgs a) {
+    __shared__ uint32_t s_hist[kEvBins], s_part[kEvWaves], s_pick[2];
+    const int tid = threadIdx.x;
+    const int problem = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
+    const Choice c(a, problem);
+    if (!c.by_score() || (int64_t)part * kEvPartRows >= c.old)
+        return;
+    const Rows r(c, part);
+    Digits d;
+    d.left = c.k;
+    if constexpr (LEVEL == 2)
+        d.take(0, a.picks[problem * 2], a.picks[problem * 2 + 1]);
+    if constexpr (LEVEL > 0) {
+        const Bins w(a, c, LEVEL - 1, problem, part);
+        pick_bin(w.c0, w.c1, d.left, s_part, s_pick);
+        if (LEVEL == 1 && part == 0 && tid < 2)
+            a.picks[problem * 2 + tid] = s_pick[tid];
+        const Digits last = d;
+        d.take(LEVEL - 1, s_pick[0], s_pick[1]);
+        // the part's rows above it
+        uint32_t gt = 0, total;
+#pragma unroll
+        for (int j = 0; j < kEvPer; j++) {
+            const uint32_t key = score_key(r.x[j]);
+            gt += r.in(j) && (key & last.mask) == last.prefix && (key & d.mask) > d.prefix;
         }
+        block_scan(gt, s_part, total);
+        if (tid == 0) {
+            uint32_t *above = a.above + (int64_t)problem * a.parts + part;
+            *above = (LEVEL == 1 ? 0u : *above) + total;
+        }
+    }
+    count_digit(r, d, LEVEL, s_hist);
+    hist_of(a, LEVEL, problem, part)[kEvBins / 2 - 1 - tid] =
+        s_hist[kEvBins - 1 - 2 * tid] << 16 | s_hist[kEvBins - 2 - 2 * tid];
+    if (LEVEL == 2 && part == 0 && tid < 2)
+        a.picks[a.num_seqs * a.hkv * 2 + problem * 2 + tid] = s_pick[tid];
+}
+
+__global__ __launch_bounds__(kEvThreads) void evict_rank_kernel(const EvictArgs a) {
+    __shared__ uint32_t s_part[kEvWaves], s_pick[2];
+    const int tid = threadIdx.x;
+    const int problem = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
+    const Choice c(a, problem);
+    const uint32_t off = place_recent(a, c, part, a.parts, s_part);
+    if (c.k == 0 || (int64_t)part * kEvPartRows >= c.old)
+        return;
+    const Rows r(c, part);
+    Digits d;
+    uint32_t gt0 = 0, eq0 = 0;
+    if (c.by_score()) {
+        const uint32_t *picks = a.picks + problem * 2;
+        d.take(0, picks[0], picks[1]);
+        picks += a.num_seqs * a.hkv * 2;
+        d.take(1, picks[0], picks[1]);
+        const Bins w(a, c, 2, problem, part);
+        pick_bin(w.c0, w.c1, d.left, s_part, s_pick);
+        // rows of the parts before this one: above the pick of each digit,
+        // and equal to the pivot
+        const uint32_t b0 = kEvBins - 1 - 2 * tid, bin = s_pick[0];
+        uint32_t gt = (b0 > bin ? w.before0 : 0u) + (b0 - 1 > bin ? w.before1 : 0u);
+        for (int i = tid; i < part; i += kEvThreads)
+            gt += a.above[(int64_t)problem * a.parts + i];
+        block_scan(gt, s_part, gt0);
+        block_scan(b0 == bin ? w.before0 : b0 - 1 == bin ? w.before1 : 0u, s_part, eq0);
+        d.take(2, bin, s_pick[1]);
+    } else {
+        gt0 = (uint32_t)part * kEvPartRows;
+    }
+    place(a, c, r, c.k == c.old, d.prefix, d.left, gt0, eq0, off, s_part);
 }
 
 template <int D>
@@ -158,8 +337,24 @@ __global__ __launch_bounds__(256) void evict_copy_kernel(const EvictArgs a) {
 }  // namespace
 
 hipError_t launch_cache_evict(const EvictArgs &a, hipStream_t s) {
-    hipLaunchKernelGGL(evict_select_kernel, dim3(a.num_seqs * a.hkv), dim3(kEvThreads), 0, s, a);
-    hipError_t e = hipGetLastError();
+    const dim3 grid_s(a.num_seqs * a.hkv * a.parts), block(kEvThreads);
+    hipError_t e;
+    if (a.parts == 1) {
+        hipLaunchKernelGGL(evict_select_kernel, grid_s, block, 0, s, a);
+        e = hipGetLastError();
+    } else {
+        hipLaunchKernelGGL((evict_hist_kernel<0>), grid_s, block, 0, s, a);
+        if ((e = hipGetLastError()) != hipSuccess)
+            return e;
+        hipLaunchKernelGGL((evict_hist_kernel<1>), grid_s, block, 0, s, a);
+        if ((e = hipGetLastError()) != hipSuccess)
+            return e;
+        hipLaunchKernelGGL((evict_hist_kernel<2>), grid_s, block, 0, s, a);
+        if ((e = hipGetLastError()) != hipSuccess)
+            return e;
+        hipLaunchKernelGGL(evict_rank_kernel, grid_s, block, 0, s, a);
+        e = hipGetLastError();
+    }
     if (e != hipSuccess || (!a.in[0] && !a.in[2]) || a.cap == 0)
         return e;
     const int rows = 256 / (a.head_dim / 8);               // per workgroup

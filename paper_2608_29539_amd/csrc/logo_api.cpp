@@ -475,6 +475,24 @@ StepScorePlan step_score_plan(const logo_problem *p) {
     return d;
 }
 
+struct EvictPlan {
+    long long parts, items;
+    size_t picks, above, total;
+};
+EvictPlan evict_plan(const logo_problem *p) {
+    EvictPlan d;
+    const size_t problems = (size_t)p->num_seqs * p->num_kv_heads;
+    d.parts = std::max(1LL, ((long long)p->max_seqlen + kEvPartRows - 1) / kEvPartRows);
+    d.items = (long long)problems * d.parts;
+    d.picks = d.above = d.total = 0;
+    if (d.parts > 1) {
+        d.picks = align_up(sizeof(uint32_t) * 2 * 1024 * problems * d.parts);
+        d.above = d.picks + align_up(sizeof(uint32_t) * 4 * problems);
+        d.total = d.above + align_up(sizeof(uint32_t) * problems * d.parts);
+    }
+    return d;
+}
+
 int64_t keep_capacity(const logo_problem *p, int32_t budget) {
     if (!p->cu_seqlens_host)
         return std::min<int64_t>(p->total_tokens, (int64_t)p->num_seqs * budget);
@@ -1103,7 +1121,7 @@ size_t logo_workspace_bytes(const logo_problem *p, int entry, int32_t sel_capaci
     case LOGO_ENTRY_GLOBAL_BWD: return global_bwd_ws(p, cap).total;
     case LOGO_ENTRY_CACHE_SCORE: return score_plan(p, cap).total;
     case LOGO_ENTRY_DECODE_SCORE: return step_score_plan(p).total;
-    case LOGO_ENTRY_CACHE_EVICT:
+    case LOGO_ENTRY_CACHE_EVICT: return evict_plan(p).total;
     case LOGO_ENTRY_LOCAL:
     case LOGO_ENTRY_COMBINE:
     case LOGO_ENTRY_DENSE: return 0;
@@ -1976,11 +1994,12 @@ logo_status logo_cache_evict(const logo_problem *p, const float *score, int32_t 
         return LOGO_ERR_NULL;
     if (capacity < keep_capacity(p, budget))
         return LOGO_ERR_SHAPE;
-    if ((long long)p->num_seqs * p->num_kv_heads >= (1LL << 31) ||
+    const EvictPlan d = evict_plan(p);
+    if (d.items >= (1LL << 31) || (long long)p->num_seqs * p->num_kv_heads >= (1LL << 29) ||
         (long long)capacity * p->num_kv_heads * (p->head_dim / 8) / 256 >= (1LL << 31) - 1)
         return LOGO_ERR_UNSUPPORTED;
-    (void)ws;                                    // (none needed)
-    (void)ws_bytes;
+    if ((st = check_ws(ws, ws_bytes, d.total)) != LOGO_OK)
+        return st;
     EvictArgs a;
     std::memset(&a, 0, sizeof a);
     a.score = score;
@@ -1999,6 +2018,10 @@ logo_status logo_cache_evict(const logo_problem *p, const float *score, int32_t 
     a.score_out = score_out;
     a.keep_idx = keep_idx;
     a.cu_keep = cu_keep;
+    a.parts = (int32_t)d.parts;
+    a.hist = (uint32_t *)ws;
+    a.picks = (uint32_t *)((char *)ws + d.picks);
+    a.above = (uint32_t *)((char *)ws + d.above);
     hipStream_t s = (hipStream_t)stream;
     return hip_status(launch_cache_evict(a, s), s);
 }

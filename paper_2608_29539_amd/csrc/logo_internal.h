@@ -319,7 +319,13 @@ struct EvictArgs {
     uint16_t *out[4];
     float *score_out;                        // [Hkv][cap]
     int32_t *keep_idx, *cu_keep;             // [Hkv][cap], [B + 1]
+    // caches of more than kEvPartRows rows, in `parts` parts: two digits'
+    // histograms [2][B Hkv][parts][1024], two picks [2][B Hkv][2], rows above
+    // them [B Hkv][parts]
+    int32_t parts;
+    uint32_t *hist, *picks, *above;
 };
+constexpr int kEvPartRows = 8192;
 hipError_t launch_cache_evict(const EvictArgs &a, hipStream_t s);
 
 // Gate projection and branch transforms (transform.hip).  kind 0 = LP
