@@ -36,30 +36,52 @@ __device__ __forceinline__ uint32_t score_key(float x) {
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// Exclusive prefix of v over the workgroup, and the total.
-__device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t *s_part, uint32_t &total) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    uint32_t incl = v;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const uint32_t x = __shfl_up(incl, d, 64);
-        if (lane >= d)
-            incl += x;
-    }
-    if (lane == 63)
-        s_part[wave] = incl;
-    __syncthreads();
-    uint32_t before = 0;
-    total = 0;
-#pragma unroll
-    for (int i = 0; i < kEvWaves; i++) {
-        const uint32_t x = s_part[i];
-        before += i < wave ? x : 0;
-        total += x;
-    }
-    __syncthreads();
-    return before + incl - v;
+// Inclusive prefix over the wave's lanes, in the vector unit: lanes 1, 2, 4 and
+// 8 to the left within rows of 16, then the last lanes of the rows before.
+template <int Ctrl, int RowMask>
+__device__ __forceinline__ uint32_t dpp_u(uint32_t x) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, Ctrl, RowMask, 0xF, false);
 }
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
+    x += dpp_u<0x111, 0xF>(x);   // row_shr:1
+    x += dpp_u<0x112, 0xF>(x);
+    x += dpp_u<0x114, 0xF>(x);
+    x += dpp_u<0x118, 0xF>(x);
+    x += dpp_u<0x142, 0xA>(x);   // row_bcast:15 into rows 1 and 3
+    x += dpp_u<0x143, 0xC>(x);   // row_bcast:31 into rows 2 and 3
+    return x;
+}
+
+// What the waves exchange: sums of theirs in turn in two places, so that a
+// scan needs one barrier (two scans later every wave has read the first).
+struct WaveSums {
+    uint32_t (*part)[kEvWaves];                            // [2] in LDS
+    int at = 0;
+    // (sum over the waves before this one, over all of them) of a value that
+    // lane 63 of each wave gives
+    __device__ __forceinline__ uint32_t exchange(uint32_t v, uint32_t &total) {
+        const int wave = threadIdx.x >> 6;
+        uint32_t *p = part[at];
+        at ^= 1;
+        if ((threadIdx.x & 63) == 63)
+            p[wave] = v;
+        __syncthreads();
+        uint32_t before = 0;
+        total = 0;
+#pragma unroll
+        for (int i = 0; i < kEvWaves; i++) {
+            const uint32_t x = p[i];
+            before += i < wave ? x : 0;
+            total += x;
+        }
+        return before;
+    }
+    // exclusive prefix of v over the workgroup, and the total
+    __device__ __forceinline__ uint32_t scan(uint32_t v, uint32_t &total) {
+        const uint32_t incl = wave_scan(v);
+        return exchange(incl, total) + incl - v;
+    }
+};
 
 // One (sequence, KV head): n rows stay of L, k of the first `old` by score.
 struct Choice {
@@ -125,10 +147,10 @@ __device__ __forceinline__ void count_digit(const Rows &r, const Digits &d, int 
 
 // The bin in which the `left`-th largest lies, from this thread's bins 2047 -
 // 2 tid (c0) and 2046 - 2 tid (c1); s_pick: the bin and how many of it stay.
-__device__ __forceinline__ void pick_bin(uint32_t c0, uint32_t c1, uint32_t left, uint32_t *s_part,
+__device__ __forceinline__ void pick_bin(uint32_t c0, uint32_t c1, uint32_t left, WaveSums &sums,
                                          uint32_t *s_pick) {
     uint32_t total;
-    const uint32_t above = block_scan(c0 + c1, s_part, total);
+    const uint32_t above = sums.scan(c0 + c1, total);
     if (above < left && left <= above + c0 + c1) {
         const bool first = left <= above + c0;
         s_pick[0] = kEvBins - 1 - 2 * threadIdx.x - (first ? 0 : 1);
@@ -138,50 +160,58 @@ __device__ __forceinline__ void pick_bin(uint32_t c0, uint32_t c1, uint32_t left
 }
 
 // Places of a part's rows: all of them, or those above the pivot and the
-// first `need` equal to it; gt0, eq0: such rows before the part.
+// first `need` equal to it; gt0, eq0: such rows before the part.  The masks of
+// 64 rows stay in scalar registers between the count and the placing.
 __device__ __forceinline__ void place(const EvictArgs &a, const Choice &c, const Rows &r, bool all,
                                       uint32_t pivot, uint32_t need, uint32_t gt0, uint32_t eq0,
-                                      uint32_t off, uint32_t *s_part) {
-    const int lane = threadIdx.x & 63;
-    const uint64_t below = (1ull << lane) - 1;
+                                      uint32_t off, WaveSums &sums) {
+    uint64_t gm[kEvPer], em[kEvPer];
     uint32_t gt = 0, eq = 0;                               // of this wave
+    const int left = c.old - uni(r.first);                 // (lane 0's row)
 #pragma unroll
     for (int j = 0; j < kEvPer; j++) {
+        const int n = left - j * 64;
+        const uint64_t real = n >= 64 ? ~0ull : n > 0 ? (1ull << n) - 1 : 0ull;
         const uint32_t key = score_key(r.x[j]);
-        gt += (uint32_t)__popcll(__ballot(r.in(j) && (all || key > pivot)));
-        eq += (uint32_t)__popcll(__ballot(r.in(j) && !all && key == pivot));
+        gm[j] = real & (all ? ~0ull : __ballot(key > pivot));
+        em[j] = real & (all ? 0ull : __ballot(key == pivot));
+        gt += (uint32_t)__popcll(gm[j]);
+        eq += (uint32_t)__popcll(em[j]);
     }
     uint32_t total;
-    const uint32_t ex = block_scan(lane == 0 ? gt | eq << 16 : 0u, s_part, total);
-    gt0 += __shfl(ex, 0, 64) & 0xFFFFu;
-    eq0 += __shfl(ex, 0, 64) >> 16;
-    const int64_t out = (int64_t)c.h * a.cap + off;
+    const uint32_t ex = uni(sums.exchange(gt | eq << 16, total));
+    gt0 = uni(gt0) + (ex & 0xFFFFu);
+    eq0 = uni(eq0) + (ex >> 16);
     const int room = a.cap - (int)off;                     // (n, for a capacity as documented)
+    int32_t *idx = a.keep_idx + (int64_t)c.h * a.cap + off;
+    float *sc = a.score_out + (int64_t)c.h * a.cap + off;
+    auto lower = [](uint64_t mask) {                       // bits below this lane
+        return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32),
+                                         __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+    };
+    const uint64_t me = 1ull << (threadIdx.x & 63);
 #pragma unroll
     for (int j = 0; j < kEvPer; j++) {
-        const uint32_t key = score_key(r.x[j]);
-        const bool g = r.in(j) && (all || key > pivot), e = r.in(j) && !all && key == pivot;
-        const uint64_t gm = __ballot(g), em = __ballot(e);
-        const uint32_t eb = eq0 + (uint32_t)__popcll(em & below);
-        const uint32_t at = gt0 + (uint32_t)__popcll(gm & below) + min(eb, need);
-        if ((g || (e && eb < need)) && (int)at < room) {
-            a.keep_idx[out + at] = c.base + r.row(j);
-            a.score_out[out + at] = r.x[j];
+        const uint32_t eb = eq0 + lower(em[j]);
+        const uint32_t at = gt0 + lower(gm[j]) + min(eb, need);
+        if (((gm[j] & me) || ((em[j] & me) && eb < need)) && (int)at < room) {
+            idx[at] = c.base + r.row(j);
+            sc[at] = r.x[j];
         }
-        gt0 += (uint32_t)__popcll(gm);
-        eq0 += (uint32_t)__popcll(em);
+        gt0 += (uint32_t)__popcll(gm[j]);
+        eq0 += (uint32_t)__popcll(em[j]);
     }
 }
 
 // Rows that the sequences before this one keep; cu_keep; the newest rows, of
 // which workgroup `part` of `parts` places its share.
 __device__ __forceinline__ uint32_t place_recent(const EvictArgs &a, const Choice &c, int part,
-                                                 int parts, uint32_t *s_part) {
+                                                 int parts) {
     const int tid = threadIdx.x;
-    uint32_t mine = 0, off;
-    for (int i = tid; i < c.b; i += kEvThreads)
+    uint32_t mine = 0;                                     // (every wave adds them up itself)
+    for (int i = tid & 63; i < c.b; i += 64)
         mine += min(a.cu[i + 1] - a.cu[i], a.budget);
-    block_scan(mine, s_part, off);
+    const uint32_t off = __builtin_amdgcn_readlane(wave_scan(mine), 63);
     if (c.h == 0 && part == 0 && tid == 0) {
         if (c.b == 0)
             a.cu_keep[0] = 0;
@@ -197,24 +227,25 @@ __device__ __forceinline__ uint32_t place_recent(const EvictArgs &a, const Choic
 }
 
 __global__ __launch_bounds__(kEvThreads) void evict_select_kernel(const EvictArgs a) {
-    __shared__ uint32_t s_hist[kEvBins], s_part[kEvWaves], s_pick[2];
+    __shared__ uint32_t s_hist[kEvBins], s_part[2][kEvWaves], s_pick[2];
     const int tid = threadIdx.x;
+    WaveSums sums{s_part};
     const Choice c(a, blockIdx.x);
     const Rows r(c, 0);
-    const uint32_t off = place_recent(a, c, 0, 1, s_part);
+    const uint32_t off = place_recent(a, c, 0, 1);
     Digits d;
     d.left = c.k;
     if (c.by_score()) {
 #pragma unroll 1
         for (int level = 0; level < 3; level++) {
             count_digit(r, d, level, s_hist);
-            pick_bin(s_hist[kEvBins - 1 - 2 * tid], s_hist[kEvBins - 2 - 2 * tid], d.left, s_part,
+            pick_bin(s_hist[kEvBins - 1 - 2 * tid], s_hist[kEvBins - 2 - 2 * tid], d.left, sums,
                      s_pick);
             d.take(level, s_pick[0], s_pick[1]);
         }
     }
     if (c.k > 0)
-        place(a, c, r, c.k == c.old, d.prefix, d.left, 0, 0, off, s_part);
+        place(a, c, r, c.k == c.old, d.prefix, d.left, 0, 0, off, sums);
 }
 
 // Two 16-bit bins per word: word 1023 - t holds thread t's bins.
@@ -246,8 +277,9 @@ struct Bins {
 // rows above the last pick are counted, and its digit LEVEL.
 template <int LEVEL>
 __global__ __launch_bounds__(kEvThreads) void evict_hist_kernel(const EvictArgs a) {
-    __shared__ uint32_t s_hist[kEvBins], s_part[kEvWaves], s_pick[2];
+    __shared__ uint32_t s_hist[kEvBins], s_part[2][kEvWaves], s_pick[2];
     const int tid = threadIdx.x;
+    WaveSums sums{s_part};
     const int problem = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
     const Choice c(a, problem);
     if (!c.by_score() || (int64_t)part * kEvPartRows >= c.old)
@@ -259,7 +291,7 @@ __global__ __launch_bounds__(kEvThreads) void evict_hist_kernel(const EvictArgs 
         d.take(0, a.picks[problem * 2], a.picks[problem * 2 + 1]);
     if constexpr (LEVEL > 0) {
         const Bins w(a, c, LEVEL - 1, problem, part);
-        pick_bin(w.c0, w.c1, d.left, s_part, s_pick);
+        pick_bin(w.c0, w.c1, d.left, sums, s_pick);
         if (LEVEL == 1 && part == 0 && tid < 2)
             a.picks[problem * 2 + tid] = s_pick[tid];
         const Digits last = d;
@@ -269,9 +301,10 @@ __global__ __launch_bounds__(kEvThreads) void evict_hist_kernel(const EvictArgs 
 #pragma unroll
         for (int j = 0; j < kEvPer; j++) {
             const uint32_t key = score_key(r.x[j]);
-            gt += r.in(j) && (key & last.mask) == last.prefix && (key & d.mask) > d.prefix;
+            gt += (uint32_t)__popcll(__ballot(r.in(j) && (key & last.mask) == last.prefix &&
+                                              (key & d.mask) > d.prefix));
         }
-        block_scan(gt, s_part, total);
+        sums.exchange(gt, total);
         if (tid == 0) {
             uint32_t *above = a.above + (int64_t)problem * a.parts + part;
             *above = (LEVEL == 1 ? 0u : *above) + total;
@@ -285,11 +318,12 @@ __global__ __launch_bounds__(kEvThreads) void evict_hist_kernel(const EvictArgs 
 }
 
 __global__ __launch_bounds__(kEvThreads) void evict_rank_kernel(const EvictArgs a) {
-    __shared__ uint32_t s_part[kEvWaves], s_pick[2];
+    __shared__ uint32_t s_part[2][kEvWaves], s_pick[2];
     const int tid = threadIdx.x;
+    WaveSums sums{s_part};
     const int problem = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
     const Choice c(a, problem);
-    const uint32_t off = place_recent(a, c, part, a.parts, s_part);
+    const uint32_t off = place_recent(a, c, part, a.parts);
     if (c.k == 0 || (int64_t)part * kEvPartRows >= c.old)
         return;
     const Rows r(c, part);
@@ -301,20 +335,20 @@ __global__ __launch_bounds__(kEvThreads) void evict_rank_kernel(const EvictArgs 
         picks += a.num_seqs * a.hkv * 2;
         d.take(1, picks[0], picks[1]);
         const Bins w(a, c, 2, problem, part);
-        pick_bin(w.c0, w.c1, d.left, s_part, s_pick);
+        pick_bin(w.c0, w.c1, d.left, sums, s_pick);
         // rows of the parts before this one: above the pick of each digit,
         // and equal to the pivot
         const uint32_t b0 = kEvBins - 1 - 2 * tid, bin = s_pick[0];
         uint32_t gt = (b0 > bin ? w.before0 : 0u) + (b0 - 1 > bin ? w.before1 : 0u);
         for (int i = tid; i < part; i += kEvThreads)
             gt += a.above[(int64_t)problem * a.parts + i];
-        block_scan(gt, s_part, gt0);
-        block_scan(b0 == bin ? w.before0 : b0 - 1 == bin ? w.before1 : 0u, s_part, eq0);
+        sums.scan(gt, gt0);
+        sums.scan(b0 == bin ? w.before0 : b0 - 1 == bin ? w.before1 : 0u, eq0);
         d.take(2, bin, s_pick[1]);
     } else {
         gt0 = (uint32_t)part * kEvPartRows;
     }
-    place(a, c, r, c.k == c.old, d.prefix, d.left, gt0, eq0, off, s_part);
+    place(a, c, r, c.k == c.old, d.prefix, d.left, gt0, eq0, off, sums);
 }
 
 template <int D>
