@@ -102,5 +102,14 @@ __device__ __forceinline__ bf16x8 read_vt_frag(const uint16_t *vrow_lane, int ro
     return lds_tr_pair(vrow_lane, vrow_lane + 8 * row_stride);
 }
 
+// Unpadded rows of D / 8 16-byte pieces: piece c of row r is stored at
+// c ^ piece_swz(r), so that the 16-byte reads of one piece from 16 rows hit
+// distinct banks (rows of D = 64 fill half of the 256-byte bank window: the
+// two rows that share one take the same permutation).
+template <int D>
+__device__ __forceinline__ constexpr int piece_swz(int r) {
+    return D == 128 ? r % 16 : (r / 2) % 8;
+}
+
 }  // namespace
 }  // namespace logo

@@ -193,29 +193,11 @@ __global__ __launch_bounds__(kScoreThreads, 2) void score_lse_kernel(const Score
 // through LDS, kScoreRows at a time in two buffers filled by direct loads: a
 // step has the next one's rows on their way while it multiplies its own, and
 // the addresses, positions and lse of the one after that, so that a step waits
-// for no chain of loads.  A row's 16-byte pieces are permuted (piece c of row r
-// is at c ^ (r % pieces)) so that the fragment reads of 16 rows hit distinct
-// banks.  Each Q fragment feeds two products (the wave's two blocks of 32
+// for no chain of loads.  A row's 16-byte pieces are permuted (piece_swz).  Each Q fragment feeds two products (the wave's two blocks of 32
 // keys), and the exponentials of one block of rows are issued between the
 // products of the next.
 // ---------------------------------------------------------------------------
 constexpr int kScoreRows = 128;
-
-// One 16-byte-per-lane load from a lane's own address to LDS (lane i writes
-// the 16 bytes at lds + 16 i); see lds_load16_at.
-__device__ __forceinline__ void lds_gather16(const void *src, uint32_t lds) {
-    const uint32_t lds_addr = __builtin_amdgcn_readfirstlane(lds);
-    uint32_t saved;
-    asm volatile(
-        "s_mov_b32 %0, m0\n\t"
-        "s_mov_b32 m0, %1\n\t"
-        "s_nop 0\n\t"
-        "global_load_lds_dwordx4 %2, off\n\t"
-        "s_mov_b32 m0, %0"
-        : "=&s"(saved)
-        : "s"(lds_addr), "v"(src)
-        : "memory");
-}
 
 // First rank in [lo, hi) whose token is at or past `tok` (tokens ascend):
 // every lane probes one of 64 equally spaced ranks.
@@ -350,7 +332,7 @@ __global__ __launch_bounds__(kScoreThreads, 2) void score_kernel(const ScoreArgs
 #pragma unroll
         for (int i = 0; i < kLoads; i++) {
             const int ld = i * kScoreWaves + wave, row = ld * kRowsPer + lane / kPc;
-            lds_gather16(s_row[step % 3][row] + ((lane % kPc) ^ (row % kPc)) * 8, dst + ld * 1024);
+            lds_gather16(s_row[step % 3][row] + ((lane % kPc) ^ piece_swz<D>(row)) * 8, dst + ld * 1024);
         }
     };
     float sum[2] = {0.f, 0.f};
@@ -380,7 +362,7 @@ __global__ __launch_bounds__(kScoreThreads, 2) void score_kernel(const ScoreArgs
 #pragma unroll
             for (int ss = 0; ss < D / 16; ss++) {
                 const bf16x8 qf =
-                    *(const bf16x8 *)&q[row * D + (((ss * 2 + g) ^ (m % kPc)) * 8)];
+                    *(const bf16x8 *)&q[row * D + (((ss * 2 + g) ^ piece_swz<D>(m)) * 8)];
 #pragma unroll
                 for (int kb = 0; kb < 2; kb++)
                     s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf, kf[kb][ss], s[kb], 0, 0, 0);
@@ -463,7 +445,7 @@ __global__ __launch_bounds__(kScoreThreads, 2) void score_kernel(const ScoreArgs
 //
 // Bound by reading K.  Each wave streams keys of its own, 16 at a time, through
 // a ring of slots in LDS (32 KB) filled by direct loads, whose lanes read
-// whole rows (a row's 16-byte pieces permuted as in score_kernel); no barrier,
+// whole rows (their pieces permuted, piece_swz); no barrier,
 // a wave waits for its own oldest slots.  Workgroups of two waves, so that two
 // of them share a CU's LDS and one's start and end hide behind the other.
 // ---------------------------------------------------------------------------
@@ -514,7 +496,7 @@ __global__ __launch_bounds__(kStepWaves * 64) void step_logits_kernel(const Step
         for (int x = 0; x < kLoads; x++) {
             const int row = x * (16 / kLoads) + lane / kPc;
             const int key = min(w0 + i * 16 + row, w1 - 1);
-            lds_gather16(kb + key * stride + ((lane % kPc) ^ (row % kPc)) * 8, dst + x * 1024);
+            lds_gather16(kb + key * stride + ((lane % kPc) ^ piece_swz<D>(row)) * 8, dst + x * 1024);
         }
     };
     const int nh = min(4 * P, G - hb * 4 * P), h0 = kvh * G + hb * 4 * P;
@@ -558,7 +540,7 @@ __global__ __launch_bounds__(kStepWaves * 64) void step_logits_kernel(const Step
 #pragma unroll
             for (int x = 0; x < D / 32; x++) {
                 const bf16x8 kf =
-                    *(const bf16x8 *)&t[n * D + (((x * 4 + kg) ^ (n % kPc)) * 8)];
+                    *(const bf16x8 *)&t[n * D + (((x * 4 + kg) ^ piece_swz<D>(n)) * 8)];
                 s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[x], kf, s, 0, 0, 0);
             }
             // keys 16 j .. + 15 belong to copy j % kCopies

@@ -19,10 +19,7 @@
 //                          local and of the global branch (rows: the group's
 //                          sequences whose window reaches it, the selected
 //                          ones) and the sequence's own part of either (rows:
-//                          the heads of one sequence).  Four waves of 32 rows;
-//                          with 64 rows or fewer two waves take the keys of a
-//                          tile by halves.  K / V tiles of 64 keys go to LDS
-//                          directly, one tile ahead.
+//                          the heads of one sequence).  Four waves of 32 rows.
 //   prefix_combine_kernel  joins the chunks of each (sequence, head), applies
 //                          ContextNorm and the fusion, rounds once to bf16.
 //
@@ -39,6 +36,38 @@ namespace {
 
 constexpr int kPfWaves = kPrefixThreads / 64;
 constexpr float kLazyP = 8.f;               // exp2-domain headroom of the running max
+
+// The larger of two: the middle of them and +inf (fmaxf makes the compiler
+// quiet its operands first, an instruction each).
+__device__ __forceinline__ float max2(float a, float b) {
+    return __builtin_amdgcn_fmed3f(a, b, __builtin_inff());
+}
+
+// Over the lanes l, l ^ 16, l ^ 32 and l ^ 48.
+__device__ __forceinline__ float quad_max(float x) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return pair_max(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+__device__ __forceinline__ float quad_sum(float x) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return pair_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
+
+// Largest over the wave, in every lane.
+template <int Ctrl>
+__device__ __forceinline__ int dpp_max(int x) {
+    return max(x, __builtin_amdgcn_update_dpp(x, x, Ctrl, 0xF, 0xF, false));
+}
+__device__ __forceinline__ int wave_max(int x) {
+    x = dpp_max<0x128>(x);   // row_ror:8
+    x = dpp_max<0x124>(x);   // row_ror:4
+    x = dpp_max<0x4E>(x);    // quad_perm [2,3,0,1]
+    x = dpp_max<0xB1>(x);    // quad_perm [1,0,3,2]
+    const auto r = __builtin_amdgcn_permlane16_swap((uint32_t)x, (uint32_t)x, false, false);
+    x = max((int)r[0], (int)r[1]);
+    const auto q = __builtin_amdgcn_permlane32_swap((uint32_t)x, (uint32_t)x, false, false);
+    return max((int)q[0], (int)q[1]);
+}
 
 // Kinds of key range (the order of the work items).
 enum { kPfxGlobal = 0, kOwnGlobal = 1, kPfxLocal = 2, kOwnLocal = 3 };
@@ -62,16 +91,20 @@ __device__ __forceinline__ int chunk_base(const PrefixArgs &a, int kind, int len
     return kind == kPfxLocal || kind == kOwnLocal ? max(0, len - a.window) : 0;
 }
 
+// Tiles of kPfKeys keys in kPfStages buffers, loaded kPfStages - 1 ahead: with
+// two workgroups per CU at d = 128, 96 KB of K and V on their way per CU.
+constexpr int kPfKeys = 32;
+constexpr int kPfStages = 4;
 template <int D>
 struct alignas(16) PrefixSmem {
-    uint16_t k[2][kBlockN][D + kKPad];
-    uint16_t v[2][kBlockN][D];
+    uint16_t k[kPfStages][kPfKeys][D];           // pieces permuted (piece_swz)
+    uint16_t v[kPfStages][kPfKeys][D];           // segments permuted (vswz)
 };
 
 template <int D>
 __global__ __launch_bounds__(kPrefixThreads, 2) void prefix_attn_kernel(const PrefixArgs a) {
     __shared__ PrefixSmem<D> sm;
-    __shared__ int s_seq[kPrefixRows], s_cnt[kPfWaves];
+    __shared__ int s_seq[kPrefixRows], s_lo[kPrefixRows], s_hi[kPrefixRows], s_cnt[kPfWaves];
     const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6);
     const int g = lane >> 5, m = lane & 31;
 
@@ -91,26 +124,30 @@ __global__ __launch_bounds__(kPrefixThreads, 2) void prefix_attn_kernel(const Pr
     // the row tiles of one chunk run on the same XCD (workgroups go to the
     // XCDs in turn), so that the later ones find its keys in that XCD's L2
     const int tiles = own ? a.own_tiles : a.pfx_tiles;
-    const int u = item / (kQueues * tiles), rem = item % (kQueues * tiles);
-    const int t = rem / kQueues, pair = u * kQueues + rem % kQueues;
-    const int kvh = pair % a.hkv, c = (pair / a.hkv) % nch, r = pair / a.hkv / nch;
+    int t = 0, pair = item;
+    if (tiles > 1) {
+        const int u = item / (kQueues * tiles), rem = item % (kQueues * tiles);
+        t = rem / kQueues;
+        pair = u * kQueues + rem % kQueues;
+    }
+    const int pk = pair / a.hkv, kvh = pair % a.hkv, r = pk / nch, c = pk % nch;
     if (r >= (own ? a.num_seqs : a.num_prefixes))
         return;
-    const float thr = decode_threshold(a);
-    if (own && global && !(a.gate[r] > thr))
+    // (all of them read before the first is looked at)
+    const int32_t *cu = own ? a.cu : a.cu_pre;
+    const int64_t base = cu[r];
+    const int len = cu[r + 1] - (int)base;
+    const int g0 = a.cu_grp[own ? 0 : r], g1 = a.cu_grp[own ? 1 : r + 1];
+    const float thr = decode_threshold(a), gate_r = a.gate[own ? r : 0];
+    if (own && global && !(gate_r > thr))
         return;                                  // an unselected token: window only
 
     // the chunk's keys [k0, k1) and the tile's rows: s_seq[i] for the
     // sequences of ranks rank0, rank0 + 1, ... among those that see the chunk
-    const int32_t *cu = own ? a.cu : a.cu_pre;
-    const int64_t base = cu[r];
-    const int len = cu[r + 1] - (int)base;
     int k0 = chunk_base(a, kind, len) + c * kc;
     int k1 = min(len, k0 + kc);
     if (k0 >= k1)
         return;
-    const int rank0 = t * kPrefixRows / a.group;
-    int count = 0;
     if (own) {
         int lo, hi;
         key_range(a, kind, 0, len, lo, hi);
@@ -118,20 +155,67 @@ __global__ __launch_bounds__(kPrefixThreads, 2) void prefix_attn_kernel(const Pr
         k1 = min(k1, hi);
         if (k0 >= k1)
             return;
-        if (tid == 0)
-            s_seq[0] = r;
+    }
+
+    // K / V tiles: a wave's kLoads loads of each, whose lanes read whole rows
+    constexpr int kPc = D / 8, kLoads = kPfKeys * kPc / 64 / kPfWaves;
+    const uint16_t *kt = own ? (global ? a.k_g : a.k) : (global ? a.kp_g : a.kp);
+    const uint16_t *vt = own ? (global ? a.v_g : a.v) : (global ? a.vp_g : a.vp);
+    const int64_t stride = (int64_t)a.hkv * D;
+    kt += base * stride + kvh * D;
+    vt += base * stride + kvh * D;
+    // Tiles are loaded in order, so the lanes' addresses move on by one tile;
+    // keys past k1 have the last one's row (they are masked).
+    const uint16_t *kp[kLoads], *vp[kLoads];
+    int row_of[kLoads];
+#pragma unroll
+    for (int i = 0; i < kLoads; i++) {
+        const int row = ((i * kPfWaves + wave) * 64 + lane) / kPc, c16 = lane % kPc;
+        row_of[i] = row;
+        const int64_t at = (k0 + row) * stride;
+        kp[i] = kt + at + (c16 ^ piece_swz<D>(row)) * 8;
+        vp[i] = vt + at + (((c16 >> 2) ^ vswz<D>(row)) * 4 + (c16 & 3)) * 8;
+    }
+    auto stage = [&](int buf, int key) {
+        const uint32_t kd = lds_addr_of(&sm.k[buf][0][0]), vd = lds_addr_of(&sm.v[buf][0][0]);
+#pragma unroll
+        for (int i = 0; i < kLoads; i++) {
+            const int ld = i * kPfWaves + wave;
+            int64_t back = 0;
+            if (key + kPfKeys > k1)
+                back = max(key + row_of[i] - (k1 - 1), 0) * stride;
+            lds_gather16(kp[i] - back, kd + ld * 1024);
+            lds_gather16(vp[i] - back, vd + ld * 1024);
+            kp[i] += kPfKeys * stride;
+            vp[i] += kPfKeys * stride;
+        }
+    };
+    auto fill = [&]() {
+#pragma unroll
+        for (int i = 0; i < kPfStages; i++)
+            if (k0 + i * kPfKeys < k1)
+                stage(i, k0 + i * kPfKeys);
+    };
+
+    // The first tiles are on their way while the rows are listed (not for a
+    // group's later row tiles, which may have none).
+    if (t == 0)
+        fill();
+    const int rank0 = t * kPrefixRows / a.group;
+    int count = 0;
+    if (own) {
         count = 1;
-        __syncthreads();
     } else {
-        const int g0 = a.cu_grp[r], g1 = a.cu_grp[r + 1];
         const int most = (t * kPrefixRows + kPrefixRows - 1) / a.group - rank0 + 1;
         for (int c0 = g0; c0 < g1; c0 += kPrefixThreads) {
             const int b = c0 + tid;
             bool in = b < g1 && (!global || a.gate[b] > thr);
+            int lo = 0, hi = 0;
             if (in) {
-                int lo, hi;
                 key_range(a, kind, len, a.cu[b + 1] - a.cu[b], lo, hi);
-                in = max(lo, k0) < min(hi, k1);
+                lo = max(lo, k0);
+                hi = min(hi, k1);
+                in = lo < hi;
             }
             const uint64_t bal = __ballot(in);
             if (lane == 0)
@@ -146,196 +230,320 @@ __global__ __launch_bounds__(kPrefixThreads, 2) void prefix_attn_kernel(const Pr
                 at += i < wave ? n : 0;
                 count += n;
             }
-            if (in && at >= 0 && at < most)
+            if (in && at >= 0 && at < most) {
                 s_seq[at] = b;
+                s_lo[at] = lo;
+                s_hi[at] = hi;
+            }
             __syncthreads();
         }
     }
     const int64_t left = (int64_t)count * a.group - (int64_t)t * kPrefixRows;
-    if (left <= 0)
+    if (left <= 0) {
+        __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);   // (no load may outlive the workgroup's LDS)
         return;
+    }
+    if (t != 0)
+        fill();
     const int nrows = left < kPrefixRows ? (int)left : kPrefixRows;
 
-    // waves: row block rb, and with few rows the key half kg of each tile
-    const int wr = nrows > 64 ? 4 : nrows > 32 ? 2 : 1;
-    const int wk = wr == 4 ? 1 : 2;
-    const int rb = wave % wr, kg = wave / wr;
-    const bool live = kg < wk && rb * 32 < nrows;
-
-    const int row_bytes = a.hkv * D * 2;
-    const uint16_t *kt = own ? (global ? a.k_g : a.k) : (global ? a.kp_g : a.kp);
-    const uint16_t *vt = own ? (global ? a.v_g : a.v) : (global ? a.vp_g : a.vp);
-    kt += (base * a.hkv + kvh) * (int64_t)D;
-    vt += (base * a.hkv + kvh) * (int64_t)D;
-    Dma<D, kPfWaves> dma;
-    dma_plan<D, kPfWaves>(dma, wave, lane, row_bytes);
-    auto stage = [&](int buf, int key) {
-        dma_k<D, kPfWaves>(&sm.k[buf][0][0], dma, kt, k1, key, row_bytes, wave);
-        dma_v<D, kPfWaves>(&sm.v[buf][0][0], dma, vt, k1, key, row_bytes, wave);
-    };
-    stage(0, k0);
-
+    // Waves of 32 rows; with 16 rows or fewer (the heads of one sequence, a
+    // small group) every wave has all of them, and tiles of its own.
+    const bool few = nrows <= 16;
+    const int first_row = few ? 0 : wave * 32, lr = few ? lane & 15 : m;
+    const bool live = first_row < nrows;
     // this lane's query row; rows past the last repeat it and are not stored
-    const int ri = min(rb * 32 + m, nrows - 1);
-    const bool row_valid = rb * 32 + m < nrows;
-    const int flat = t * kPrefixRows + ri;
-    const int b = s_seq[flat / a.group - rank0];
+    const int ri = min(first_row + lr, nrows - 1);
+    const bool row_valid = first_row + lr < nrows;
+    const int flat = t * kPrefixRows + ri, rank = flat / a.group - rank0;
+    const int b = own ? r : s_seq[rank];
+    const int lo = own ? k0 : s_lo[rank], hi = own ? k1 : s_hi[rank];
     const int head = kvh * a.group + flat % a.group;
-    const uint16_t *qp = (global ? a.q_g : a.q) + ((int64_t)b * a.hq + head) * D + g * 8;
-    bf16x8 qf[D / 16];
-#pragma unroll
-    for (int s = 0; s < D / 16; s++)
-        qf[s] = *(const bf16x8 *)(qp + s * 16);
-    int lo, hi;
-    {
-        const int S = a.cu[b + 1] - a.cu[b];
-        key_range(a, kind, len, own ? len : S, lo, hi);
-        lo = max(lo, k0);
-        hi = min(hi, k1);
-    }
+    const uint16_t *qp = (global ? a.q_g : a.q) + ((int64_t)b * a.hq + head) * D;
     // keys that every row of the wave sees: tiles inside need no mask
-    int all_lo = lo, all_hi = hi;
-#pragma unroll
-    for (int sh = 1; sh < 32; sh <<= 1) {
-        all_lo = max(all_lo, __shfl_xor(all_lo, sh, 64));
-        all_hi = min(all_hi, __shfl_xor(all_hi, sh, 64));
-    }
-    all_lo = uni(all_lo);
-    all_hi = uni(all_hi);
-
-    const int vt_row = 4 * g + ((lane & 15) >> 2);
-    const int vt_col = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
-    int vt_scol[D / 32];
-#pragma unroll
-    for (int cb = 0; cb < D / 32; cb++)
-        vt_scol[cb] = (cb ^ vswz<D>(vt_row)) * 32 + vt_col;
+    const int all_lo = uni(wave_max(lo)), all_hi = -uni(wave_max(-hi));
     const float sc = a.scale_log2;
     const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
-    f32x16 acc[D / 32];
-#pragma unroll
-    for (int cb = 0; cb < D / 32; cb++)
-        acc[cb] = f32x16{};
+    const int64_t prow = ((int64_t)(a.slot0[kind] + c) * a.num_seqs + b) * a.hq + head;
     float m_ref = kNegInf, l_run = 0.f;
-
-    // One wave's share of the tile in buffer `buf`, keys key0 + 32 sb0 ...:
-    // N blocks of 32 keys.
-    auto step = [&](auto n_blocks, int buf, int sb0, int key0) {
-        constexpr int N = decltype(n_blocks)::value;
-        f32x16 s[N];
-#pragma unroll
-        for (int sb = 0; sb < N; sb++)
-            s[sb] = f32x16{};
-#pragma unroll
-        for (int ss = 0; ss < D / 16; ss++)
-#pragma unroll
-            for (int sb = 0; sb < N; sb++) {
-                const bf16x8 kf = *(const bf16x8 *)&sm.k[buf][(sb0 + sb) * 32 + m][ss * 16 + g * 8];
-                s[sb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[ss], s[sb], 0, 0, 0);
-            }
-        if (key0 + sb0 * 32 < all_lo || key0 + (sb0 + N) * 32 > all_hi) {
-#pragma unroll
-            for (int sb = 0; sb < N; sb++)
-#pragma unroll
-                for (int i = 0; i < 16; i++) {
-                    const int key = key0 + (sb0 + sb) * 32 + (i >> 2) * 8 + g * 4 + (i & 3);
-                    if (key < lo || key >= hi)
-                        s[sb][i] = kNegInf;
-                }
-        }
-        float mx = kNegInf;
-#pragma unroll
-        for (int sb = 0; sb < N; sb++)
-#pragma unroll
-            for (int i = 0; i < 16; i++)
-                mx = fmaxf(mx, s[sb][i]);
-        mx = pair_max(mx) * sc;
+    // the running max of a tile's scores moves (rescaling O and l) when it is
+    // exceeded by kLazyP; returns what the exponents subtract
+    auto rescale = [&](float mx, auto &acc) {
         const bool move = mx > m_ref + kLazyP;
         if (__builtin_amdgcn_ballot_w64(move) != 0) {
             const float m_new = move ? mx : m_ref;
             const float alpha = move ? __builtin_amdgcn_exp2f(m_ref - m_new) : 1.f;
             m_ref = m_new;
             l_run *= alpha;
-#pragma unroll
-            for (int cb = 0; cb < D / 32; cb++)
-                acc[cb] *= alpha;
+            for (auto &x : acc)
+                x *= alpha;
         }
-        const float mc = m_ref == kNegInf ? 0.f : m_ref;
-        bf16x2 pw[N][8];
-#pragma unroll
-        for (int sb = 0; sb < N; sb++)
-#pragma unroll
-            for (int i = 0; i < 16; i += 2) {
-                pw[sb][i >> 1] = cvt_bf16x2(__builtin_amdgcn_exp2f(fmaf(s[sb][i], sc, -mc)),
-                                            __builtin_amdgcn_exp2f(fmaf(s[sb][i + 1], sc, -mc)));
-                l_run = __builtin_amdgcn_fdot2_f32_bf16(pw[sb][i >> 1], ones, l_run, false);
-            }
-#pragma unroll
-        for (int sb = 0; sb < N; sb++)
-#pragma unroll
-            for (int ss = 0; ss < 2; ss++) {
-                bf16x8 pf;
-#pragma unroll
-                for (int j = 0; j < 4; j++) {
-                    pf[2 * j] = pw[sb][ss * 4 + j][0];
-                    pf[2 * j + 1] = pw[sb][ss * 4 + j][1];
-                }
-#pragma unroll
-                for (int cb = 0; cb < D / 32; cb++) {
-                    const bf16x8 vf = read_vt_frag(
-                        &sm.v[buf][(sb0 + sb) * 32 + ss * 16 + vt_row][vt_scol[cb]], D);
-                    acc[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf, acc[cb], 0, 0, 0);
-                }
-            }
+        return m_ref == kNegInf ? 0.f : m_ref;
     };
+    constexpr int kAhead = kPfStages - 1;
 
-    int buf = 0;
-    for (int key = k0; key < k1; key += kBlockN, buf ^= 1) {
-        dma_wait_barrier();                      // this tile is in, the other buffer is read
-        if (key + kBlockN < k1)
-            stage(buf ^ 1, key + kBlockN);
-        if (live) {
-            if (wk == 1)
-                step(std::integral_constant<int, 2>{}, buf, 0, key);
-            else
-                step(std::integral_constant<int, 1>{}, buf, kg, key);
+    if (few) {
+        // Wave w has tiles w, w + 4, ... in stage w of its own, which it reads
+        // into registers whole and fills again before it multiplies: no
+        // barriers, and the four waves' chains cover each other.  O^T = V^T P^T
+        // in blocks of 16 d values; lane (row lr, kg): keys 4 kg + 0..3 of the
+        // tile's halves, the product's order of keys.
+        static_assert(kPfStages == kPfWaves, "a stage per wave");
+        const int kg = lane >> 4;
+        bf16x8 qf[D / 32];
+#pragma unroll
+        for (int x = 0; x < D / 32; x++)
+            qf[x] = *(const bf16x8 *)(qp + x * 32 + kg * 8);
+        const int vt_row = 4 * kg + ((lane & 15) >> 2), vt_col = 4 * (lane & 3);
+        f32x4 acc[D / 16];
+#pragma unroll
+        for (int x = 0; x < D / 16; x++)
+            acc[x] = f32x4{};
+        // the wave's whole tile at `key`
+        constexpr int kRowsPer = 64 / kPc;       // rows per load
+        const uint32_t kd = lds_addr_of(&sm.k[wave][0][0]), vd = lds_addr_of(&sm.v[wave][0][0]);
+        auto stage_own = [&](int key) {
+            const int row0 = lane / kPc, c16 = lane % kPc;
+            const uint16_t *kr = kt + (key + row0) * stride, *vr = vt + (key + row0) * stride;
+            const bool whole = key + kPfKeys <= k1;
+#pragma unroll
+            for (int ld = 0; ld < kPfKeys / kRowsPer; ld++) {
+                const int row = ld * kRowsPer + row0;
+                int64_t at = (int64_t)ld * kRowsPer * stride;
+                if (!whole)
+                    at -= max(key + row - (k1 - 1), 0) * stride;
+                lds_gather16(kr + at + (c16 ^ piece_swz<D>(row)) * 8, kd + ld * 1024);
+                lds_gather16(vr + at + (((c16 >> 2) ^ vswz<D>(row)) * 4 + (c16 & 3)) * 8,
+                             vd + ld * 1024);
+            }
+        };
+        dma_wait_barrier();                      // the first four tiles, the queries
+#pragma unroll 1
+        for (int key = k0 + wave * kPfKeys; key < k1; key += kPfWaves * kPfKeys) {
+            __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);
+            asm volatile("" ::: "memory");
+            bf16x8 kf[2][D / 32], vf[D / 16];
+#pragma unroll
+            for (int x = 0; x < D / 32; x++)
+#pragma unroll
+                for (int h = 0; h < 2; h++) {
+                    const int row = h * 16 + lr;
+                    kf[h][x] =
+                        *(const bf16x8 *)&sm.k[wave][row][((x * 4 + kg) ^ piece_swz<D>(row)) * 8];
+                }
+#pragma unroll
+            for (int x = 0; x < D / 16; x++) {
+                const uint16_t *vr = &sm.v[wave][vt_row][((x / 2) ^ vswz<D>(vt_row)) * 32 +
+                                                         (x % 2) * 16 + vt_col];
+                vf[x] = lds_tr_pair(vr, vr + 16 * D);
+            }
+            // the stage is read before it is filled again
+            __builtin_amdgcn_s_waitcnt(kWaitLgkmcnt0);
+            asm volatile("" ::: "memory");
+            if (key + kPfWaves * kPfKeys < k1)
+                stage_own(key + kPfWaves * kPfKeys);
+            f32x4 s[2] = {};
+#pragma unroll
+            for (int x = 0; x < D / 32; x++)
+#pragma unroll
+                for (int h = 0; h < 2; h++)
+                    s[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[h][x], qf[x], s[h], 0, 0, 0);
+            if (key < all_lo || key + kPfKeys > all_hi) {
+#pragma unroll
+                for (int h = 0; h < 2; h++)
+#pragma unroll
+                    for (int i = 0; i < 4; i++) {
+                        const int j = key + h * 16 + kg * 4 + i;
+                        if (j < lo || j >= hi)
+                            s[h][i] = kNegInf;
+                    }
+            }
+            float mx = max2(max2(max2(s[0][0], s[0][1]), max2(s[0][2], s[0][3])),
+                            max2(max2(s[1][0], s[1][1]), max2(s[1][2], s[1][3])));
+            mx = quad_max(mx) * sc;
+            const float mc = rescale(mx, acc);
+            bf16x8 pf;
+#pragma unroll
+            for (int h = 0; h < 2; h++)
+#pragma unroll
+                for (int i = 0; i < 4; i += 2) {
+                    const bf16x2 p =
+                        cvt_bf16x2(__builtin_amdgcn_exp2f(fmaf(s[h][i], sc, -mc)),
+                                   __builtin_amdgcn_exp2f(fmaf(s[h][i + 1], sc, -mc)));
+                    l_run = __builtin_amdgcn_fdot2_f32_bf16(p, ones, l_run, false);
+                    pf[h * 4 + i] = p[0];
+                    pf[h * 4 + i + 1] = p[1];
+                }
+#pragma unroll
+            for (int x = 0; x < D / 16; x++)
+                acc[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[x], pf, acc[x], 0, 0, 0);
         }
+        // The waves' (O, m, l) joined through LDS (the stages are read): wave w
+        // takes its quarter of the blocks.
+        constexpr int kVals = D / 4 + 2;         // floats per lane and wave
+        static_assert(sizeof(PrefixSmem<D>) >= kPfWaves * 64 * kVals * sizeof(float), "LDS");
+        float *mine = (float *)&sm + wave * 64 * kVals + lane;
+        const float lw = quad_sum(l_run);
+        __syncthreads();
+#pragma unroll
+        for (int x = 0; x < D / 16; x++)
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+                mine[(x * 4 + i) * 64] = acc[x][i];
+        mine[D / 4 * 64] = m_ref;
+        mine[(D / 4 + 1) * 64] = lw;
+        __syncthreads();
+        const float *all = (const float *)&sm + lane;
+        float M = kNegInf, f[kPfWaves], l = 0.f;
+#pragma unroll
+        for (int w = 0; w < kPfWaves; w++) {
+            f[w] = all[(w * kVals + D / 4) * 64];
+            M = fmaxf(M, f[w]);
+        }
+        const float Mc = M == kNegInf ? 0.f : M;
+#pragma unroll
+        for (int w = 0; w < kPfWaves; w++) {
+            f[w] = __builtin_amdgcn_exp2f(f[w] - Mc);
+            l = fmaf(f[w], all[(w * kVals + D / 4 + 1) * 64], l);
+        }
+        constexpr int kOwn = D / 16 / kPfWaves;
+#pragma unroll
+        for (int x = 0; x < kOwn; x++) {
+            f32x4 o = {};
+#pragma unroll
+            for (int w = 0; w < kPfWaves; w++)
+#pragma unroll
+                for (int i = 0; i < 4; i++)
+                    o[i] = fmaf(f[w], all[(w * kVals + (wave * kOwn + x) * 4 + i) * 64], o[i]);
+            if (row_valid)
+                *(f32x4 *)(a.part + prow * D + (wave * kOwn + x) * 16 + 4 * kg) = o;
+        }
+        if (row_valid && kg == 0 && wave == 0)
+            *(f32x2 *)(a.ml + 2 * prow) = f32x2{M, l};
+        return;
     }
 
-    // The two key halves joined through LDS (the tiles are read).
-    if (wk == 2) {
-        float *other = (float *)&sm + rb * 64 * (D / 2 + 2) + lane;
-        static_assert(sizeof(PrefixSmem<D>) >= 2 * 64 * (D / 2 + 2) * sizeof(float), "LDS");
-        __syncthreads();
-        if (live && kg == 1) {
+    bf16x8 qf[D / 16];
 #pragma unroll
-            for (int cb = 0; cb < D / 32; cb++)
+    for (int s = 0; s < D / 16; s++)
+        qf[s] = *(const bf16x8 *)(qp + g * 8 + s * 16);
+    const int vt_row = 4 * g + ((lane & 15) >> 2);
+    const int vt_col = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+    int vt_scol[D / 32];
 #pragma unroll
-                for (int i = 0; i < 16; i++)
-                    other[(cb * 16 + i) * 64] = acc[cb][i];
-            other[D / 2 * 64] = m_ref;
-            other[(D / 2 + 1) * 64] = l_run;
-        }
-        __syncthreads();
-        if (!live || kg != 0)
-            return;
-        const float mo = other[D / 2 * 64], M = fmaxf(m_ref, mo);
-        const float Mc = M == kNegInf ? 0.f : M;
-        const float fa = __builtin_amdgcn_exp2f(m_ref - Mc), fb = __builtin_amdgcn_exp2f(mo - Mc);
+    for (int cb = 0; cb < D / 32; cb++)
+        vt_scol[cb] = (cb ^ vswz<D>(vt_row)) * 32 + vt_col;
+    f32x16 acc[D / 32];
+#pragma unroll
+    for (int cb = 0; cb < D / 32; cb++)
+        acc[cb] = f32x16{};
+
+    constexpr int kHalf = D / 32;
+    auto k_frags = [&](int buf, int ss0, bf16x8 (&kf)[kHalf]) {
+#pragma unroll
+        for (int i = 0; i < kHalf; i++)
+            kf[i] = *(const bf16x8 *)&sm.k[buf][m][(((ss0 + i) * 2 + g) ^ piece_swz<D>(m)) * 8];
+    };
+    auto v_frags = [&](int buf, int ss, bf16x8 (&vf)[D / 32]) {
 #pragma unroll
         for (int cb = 0; cb < D / 32; cb++)
+            vf[cb] = read_vt_frag(&sm.v[buf][ss * 16 + vt_row][vt_scol[cb]], D);
+    };
+    auto scores = [&](f32x16 s, int ss0, const bf16x8 (&kf)[kHalf]) {
 #pragma unroll
-            for (int i = 0; i < 16; i++)
-                acc[cb][i] = fmaf(acc[cb][i], fa, other[(cb * 16 + i) * 64] * fb);
-        l_run = fmaf(l_run, fa, other[(D / 2 + 1) * 64] * fb);
-        m_ref = M;
+        for (int i = 0; i < kHalf; i++)
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i], qf[ss0 + i], s, 0, 0, 0);
+        return s;
+    };
+    // Tile `buf` with its scores s; on return s has the next tile's scores,
+    // whose products are issued between this one's exponentials (past the last
+    // tile they are not used).  Fragments are read half a tile ahead of the
+    // products that take them.
+    auto step = [&](int buf, int key0, f32x16 &s) {
+        const int nbuf = (buf + 1) % kPfStages;
+        bf16x8 kf[2][kHalf], vf[2][D / 32];
+        k_frags(nbuf, 0, kf[0]);
+        __builtin_amdgcn_sched_barrier(0);
+        if (key0 < all_lo || key0 + kPfKeys > all_hi) {
+#pragma unroll
+            for (int i = 0; i < 16; i++) {
+                const int key = key0 + (i >> 2) * 8 + g * 4 + (i & 3);
+                if (key < lo || key >= hi)
+                    s[i] = kNegInf;
+            }
+        }
+        float mx[4];
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+            mx[i] = max2(max2(s[i], s[i + 4]), max2(s[i + 8], s[i + 12]));
+        const float top = pair_max(max2(max2(mx[0], mx[1]), max2(mx[2], mx[3]))) * sc;
+        const float mc = rescale(top, acc);
+        k_frags(nbuf, kHalf, kf[1]);
+        v_frags(buf, 0, vf[0]);
+        __builtin_amdgcn_sched_barrier(0);
+        f32x16 next = scores(f32x16{}, 0, kf[0]);
+        bf16x2 pw[8];
+        float l2 = 0.f;
+        auto exps = [&](int i0) {
+#pragma unroll
+            for (int i = i0; i < i0 + 8; i += 2) {
+                pw[i >> 1] = cvt_bf16x2(__builtin_amdgcn_exp2f(fmaf(s[i], sc, -mc)),
+                                        __builtin_amdgcn_exp2f(fmaf(s[i + 1], sc, -mc)));
+                float &lx = (i & 2) ? l2 : l_run;
+                lx = __builtin_amdgcn_fdot2_f32_bf16(pw[i >> 1], ones, lx, false);
+            }
+        };
+        exps(0);
+        v_frags(buf, 1, vf[1]);
+        __builtin_amdgcn_sched_barrier(0);
+        next = scores(next, kHalf, kf[1]);
+        exps(8);
+        l_run += l2;
+#pragma unroll
+        for (int ss = 0; ss < 2; ss++) {
+            bf16x8 pf;
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                pf[2 * j] = pw[ss * 4 + j][0];
+                pf[2 * j + 1] = pw[ss * 4 + j][1];
+            }
+#pragma unroll
+            for (int cb = 0; cb < D / 32; cb++)
+                acc[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[ss][cb], pf, acc[cb], 0, 0, 0);
+        }
+        s = next;
+    };
+
+    // (the queries are in before the loop, whose waits count the tiles' loads
+    // alone; the first tiles with them)
+    dma_wait_barrier();
+    f32x16 s = {};
+    if (live) {
+        bf16x8 kf[kHalf];
+        k_frags(0, 0, kf);
+        s = scores(s, 0, kf);
+        k_frags(0, kHalf, kf);
+        s = scores(s, kHalf, kf);
     }
+    int buf = 0;
+    for (int key = k0; key < k1; key += kPfKeys, buf = (buf + 1) % kPfStages) {
+        // the next tile is in, and the buffer of the one before this is read
+        if (key + (kAhead - 1) * kPfKeys < k1)
+            dma_wait_barrier_but<(kAhead - 2) * 2 * kLoads>();
+        else
+            dma_wait_barrier();
+        if (key > k0 && key + kAhead * kPfKeys < k1)
+            stage((buf + kAhead) % kPfStages, key + kAhead * kPfKeys);
+        if (live)
+            step(buf, key, s);
+    }
+
     if (!live)
         return;
     const float l = pair_sum(l_run);
     if (!row_valid)
         return;
-    const int64_t row = ((int64_t)(a.slot0[kind] + c) * a.num_seqs + b) * a.hq + head;
-    float *op = a.part + row * D + 4 * g;
+    float *op = a.part + prow * D + 4 * g;
 #pragma unroll
     for (int cb = 0; cb < D / 32; cb++)
 #pragma unroll
@@ -343,7 +551,7 @@ __global__ __launch_bounds__(kPrefixThreads, 2) void prefix_attn_kernel(const Pr
             *(f32x4 *)(op + cb * 32 + q * 8) = f32x4{acc[cb][4 * q], acc[cb][4 * q + 1],
                                                      acc[cb][4 * q + 2], acc[cb][4 * q + 3]};
     if (g == 0)
-        *(f32x2 *)(a.ml + 2 * row) = f32x2{m_ref, l};
+        *(f32x2 *)(a.ml + 2 * prow) = f32x2{m_ref, l};
 }
 
 // WPH waves per (sequence, head), four waves per workgroup; a wave's halves

@@ -385,9 +385,14 @@ struct PrefixPlan {
     size_t ml, total;
 };
 
-// Keys per chunk: the prefix's part of the global branch in about 512
-// workgroups (two per CU) over the KV heads and row tiles, at least 128 keys
-// each; the other ranges in chunks of 512 keys; at most kMaxPrefixChunks each.
+// Keys per chunk.  The prefix's part of the global branch: about 256
+// workgroups (one per CU, the other ranges' beside them) over the KV heads and
+// row tiles, at least 128 keys each; with 512 the step of 32 sequences behind
+// 16K tokens took 43 us instead of 38 (partial results, more starts), with 128
+// that of 64 behind 32K 126 instead of 87.  The sequences' own rows: 512 keys,
+// 256 where that makes fewer than 512 workgroups (23 sequences, 2 KV heads:
+// 32 and 24 us; 32 and 8: 38 and 39).  The window's part of a prefix: 256.
+// At most kMaxPrefixChunks each.
 PrefixPlan prefix_plan(const logo_problem *p, const logo_prefix *x, bool share) {
     PrefixPlan d;
     const long long G = p->num_q_heads / p->num_kv_heads, w = p->window;
@@ -397,7 +402,10 @@ PrefixPlan prefix_plan(const logo_problem *p, const logo_prefix *x, bool share) 
     const long long span[4] = {maxP, share ? (maxS > w ? maxS - w : 0) : maxS,
                                maxP < w ? maxP : w, maxS < w ? maxS : w};
     const long long work = (long long)x->total_tokens * p->num_kv_heads * d.pfx_tiles;
-    const long long want[4] = {std::max(128LL, (work + 511) / 512), 512, 512, 512};
+    const long long own_items = p->num_seqs * (long long)p->num_kv_heads * d.own_tiles *
+                                ((maxS + 511) / 512);
+    const long long own = own_items >= 512 ? 512 : 256;
+    const long long want[4] = {std::max(128LL, (work + 255) / 256), own, 256, own};
     long long slots = 0, first = 0;
     for (int i = 0; i < 4; i++) {
         long long kc = std::max(want[i], (span[i] + kMaxPrefixChunks - 1) / kMaxPrefixChunks);
@@ -406,11 +414,11 @@ PrefixPlan prefix_plan(const logo_problem *p, const logo_prefix *x, bool share) 
         d.chunks[i] = (int)((span[i] + kc - 1) / kc);
         d.slot0[i] = (int)slots;
         slots += d.chunks[i];
-        const bool own = i & 1;
-        const long long pairs = (long long)(own ? p->num_seqs : x->num_prefixes) * d.chunks[i] *
+        const bool is_own = i & 1;
+        const long long pairs = (long long)(is_own ? p->num_seqs : x->num_prefixes) * d.chunks[i] *
                                 p->num_kv_heads;
         d.first[i] = first;
-        first += (pairs + kQueues - 1) / kQueues * kQueues * (own ? d.own_tiles : d.pfx_tiles);
+        first += (pairs + kQueues - 1) / kQueues * kQueues * (is_own ? d.own_tiles : d.pfx_tiles);
     }
     d.first[4] = first;
     d.slots = (int)slots;
