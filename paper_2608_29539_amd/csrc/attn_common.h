@@ -31,6 +31,12 @@ __device__ __forceinline__ float pair_sum(float x) {
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// The larger of two: the middle of them and +inf (fmaxf makes the compiler
+// quiet its operands first, an instruction each).
+__device__ __forceinline__ float max2(float a, float b) {
+    return __builtin_amdgcn_fmed3f(a, b, __builtin_inff());
+}
+
 // Wave-uniform value, made explicit so the compiler keeps it in SGPRs.
 __device__ __forceinline__ int uni(int x) { return __builtin_amdgcn_readfirstlane(x); }
 

@@ -30,10 +30,17 @@ constexpr int kScoreWaves = kScoreThreads / 64;
 constexpr int kLseBuffers = 4;
 
 // Item t of the blocks that sequences have n(b) of each, sequence-major: its
-// sequence and block; false past the last.  Every wave searches for itself.
+// sequence and block; false past the last.  per_seq > 0: every sequence has
+// that many places (of which n(b) are blocks); else every wave searches for
+// itself.
 template <class F>
-__device__ __forceinline__ bool find_block(int t, int B, F &&n, int &b, int &j) {
+__device__ __forceinline__ bool find_block(int t, int B, int per_seq, F &&n, int &b, int &j) {
     const int lane = threadIdx.x & 63;
+    if (per_seq > 0) {
+        b = t / per_seq;
+        j = t % per_seq;
+        return b < B && j < n(b);
+    }
     int before = 0;
     for (int b0 = 0; b0 < B; b0 += 64) {
         const int c = b0 + lane < B ? n(b0 + lane) : 0;
@@ -58,7 +65,7 @@ __device__ __forceinline__ bool find_block(int t, int B, F &&n, int &b, int &j) 
 
 // The query rows of sequence b: ranks [s0, s1) of sel_idx, or its tokens.
 __device__ __forceinline__ void row_span(const ScoreArgs &a, int b, int &s0, int &s1) {
-    if (a.sel_idx) {
+    if (a.cu_sel) {
         s0 = min(a.cu_sel[b], a.cap);
         s1 = min(a.cu_sel[b + 1], a.cap);
     } else {
@@ -67,19 +74,7 @@ __device__ __forceinline__ void row_span(const ScoreArgs &a, int b, int &s0, int
     }
 }
 __device__ __forceinline__ int token_of(const ScoreArgs &a, int rank) {
-    return a.sel_idx ? a.sel_idx[rank] : rank;
-}
-
-// 32 x 32 block of scores: rows of A (16-byte fragments in LDS, `stride`
-// bf16 apart) with the B fragments in registers.
-template <int D>
-__device__ __forceinline__ f32x16 block_scores(const uint16_t *frag, const bf16x8 (&bf)[D / 16]) {
-    f32x16 s = {};
-#pragma unroll
-    for (int ss = 0; ss < D / 16; ss++)
-        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8 *)(frag + ss * 16), bf[ss], s,
-                                                    0, 0, 0);
-    return s;
+    return a.cu_sel ? a.sel_idx[rank] : rank;
 }
 
 // ---------------------------------------------------------------------------
@@ -97,7 +92,7 @@ __global__ __launch_bounds__(kScoreThreads, 2) void score_lse_kernel(const Score
     item /= a.hkv;
     const int c = item % a.lse_chunks;
     int b, t;
-    if (!find_block(item / a.lse_chunks, a.num_seqs, [&](int i) {
+    if (!find_block(item / a.lse_chunks, a.num_seqs, a.lse_per_seq, [&](int i) {
             int s0, s1;
             row_span(a, i, s0, s1);
             return (int)(((int64_t)(s1 - s0) * G + kLseRows - 1) / kLseRows);
@@ -151,10 +146,20 @@ __global__ __launch_bounds__(kScoreThreads, 2) void score_lse_kernel(const Score
         stage(key + kAhead * kBlockN, (buf + kAhead) % kLseBuffers);
         if (!live)
             continue;
-        f32x16 s[2];
+        // every fragment is on its way before the first product
+        bf16x8 kf[2][D / 16];
 #pragma unroll
         for (int sb = 0; sb < 2; sb++)
-            s[sb] = block_scores<D>(&s_k[buf][sb * 32 + m][g * 8], qf);
+#pragma unroll
+            for (int ss = 0; ss < D / 16; ss++)
+                kf[sb][ss] = *(const bf16x8 *)&s_k[buf][sb * 32 + m][ss * 16 + g * 8];
+        __builtin_amdgcn_sched_barrier(0);
+        f32x16 s[2] = {};
+#pragma unroll
+        for (int ss = 0; ss < D / 16; ss++)
+#pragma unroll
+            for (int sb = 0; sb < 2; sb++)
+                s[sb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[sb][ss], qf[ss], s[sb], 0, 0, 0);
         if (key + 63 > pos_min || key + 64 > k1) {
 #pragma unroll
             for (int sb = 0; sb < 2; sb++)
@@ -165,21 +170,22 @@ __global__ __launch_bounds__(kScoreThreads, 2) void score_lse_kernel(const Score
                         s[sb][i] = kNegInf;
                 }
         }
-        float mx = kNegInf;
+        float top[4];
 #pragma unroll
-        for (int sb = 0; sb < 2; sb++)
-#pragma unroll
-            for (int i = 0; i < 16; i++)
-                mx = fmaxf(mx, s[sb][i]);
-        mx = pair_max(mx) * a.scale_log2;
+        for (int i = 0; i < 4; i++) {
+            const float x = max2(max2(s[0][i], s[0][i + 4]), max2(s[0][i + 8], s[0][i + 12]));
+            const float y = max2(max2(s[1][i], s[1][i + 4]), max2(s[1][i + 8], s[1][i + 12]));
+            top[i] = max2(x, y);
+        }
+        const float mx = pair_max(max2(max2(top[0], top[1]), max2(top[2], top[3]))) * a.scale_log2;
         const float mn = fmaxf(mr, mx), mc = mn == kNegInf ? 0.f : mn;
-        float sum = 0.f;
+        float sum[2] = {};
 #pragma unroll
         for (int sb = 0; sb < 2; sb++)
 #pragma unroll
             for (int i = 0; i < 16; i++)
-                sum += __builtin_amdgcn_exp2f(fmaf(s[sb][i], a.scale_log2, -mc));
-        l = fmaf(l, __builtin_amdgcn_exp2f(mr - mc), sum);
+                sum[i & 1] += __builtin_amdgcn_exp2f(fmaf(s[sb][i], a.scale_log2, -mc));
+        l = fmaf(l, __builtin_amdgcn_exp2f(mr - mc), sum[0] + sum[1]);
         mr = mn;
     }
     l = pair_sum(l);
@@ -202,7 +208,7 @@ constexpr int kScoreRows = 128;
 // First rank in [lo, hi) whose token is at or past `tok` (tokens ascend):
 // every lane probes one of 64 equally spaced ranks.
 __device__ __forceinline__ int first_rank(const ScoreArgs &a, int lo, int hi, int tok) {
-    if (!a.sel_idx)
+    if (!a.cu_sel)
         return min(max(tok, lo), hi);
     const int lane = threadIdx.x & 63;
     while (lo < hi) {
@@ -234,7 +240,7 @@ __global__ __launch_bounds__(kScoreThreads, 2) void score_kernel(const ScoreArgs
     const int G = a.group;
     const int kvh = blockIdx.x % a.hkv;
     int b, jb;
-    if (!find_block(blockIdx.x / a.hkv, a.num_seqs,
+    if (!find_block(blockIdx.x / a.hkv, a.num_seqs, a.per_seq,
                     [&](int i) { return (a.cu[i + 1] - a.cu[i] + KW * 64 - 1) / (KW * 64); }, b, jb))
         return;
     const int base = a.cu[b];

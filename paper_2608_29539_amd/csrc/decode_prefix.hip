@@ -37,12 +37,6 @@ namespace {
 constexpr int kPfWaves = kPrefixThreads / 64;
 constexpr float kLazyP = 8.f;               // exp2-domain headroom of the running max
 
-// The larger of two: the middle of them and +inf (fmaxf makes the compiler
-// quiet its operands first, an instruction each).
-__device__ __forceinline__ float max2(float a, float b) {
-    return __builtin_amdgcn_fmed3f(a, b, __builtin_inff());
-}
-
 // Over the lanes l, l ^ 16, l ^ 32 and l ^ 48.
 __device__ __forceinline__ float quad_max(float x) {
     const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);

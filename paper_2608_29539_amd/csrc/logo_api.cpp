@@ -429,10 +429,21 @@ PrefixPlan prefix_plan(const logo_problem *p, const logo_prefix *x, bool share) 
 }
 
 struct ScorePlan {
-    int key_waves, lse_kc, lse_chunks;
+    int key_waves, lse_kc, lse_chunks, per_seq, lse_per_seq;
     long long items, lse_items;
     size_t total;
 };
+
+// Blocks of `block` over sequences of at most `longest` with `total` in all:
+// the same number for every sequence where that is at most twice the sum of
+// their own (a workgroup then finds its sequence by a division), else what
+// bounds the sum.
+long long score_blocks(long long total, long long longest, long long B, long long block,
+                       int &per_seq) {
+    const long long bound = total / block + B, each = (longest + block - 1) / block;
+    per_seq = each * B <= 2 * bound ? (int)each : 0;
+    return per_seq > 0 ? each * B : bound;
+}
 
 // Keys per workgroup (64, 128 or 256): the most that still makes 256
 // workgroups, one per CU.  More keys share the staged rows; fewer make up for
@@ -444,10 +455,12 @@ ScorePlan score_plan(const logo_problem *p, int32_t cap) {
     const long long N = p->total_tokens, B = p->num_seqs, H = p->num_kv_heads;
     const long long G = p->num_q_heads / p->num_kv_heads;
     d.key_waves = N * H >= 256 * 256 ? 4 : N * H >= 256 * 128 ? 2 : 1;
-    d.items = (N / (64 * d.key_waves) + B) * H;
-    const long long tiles = ((long long)cap * G) / kLseRows + B;
     const long long maxL = std::max(1, p->max_seqlen);
-    long long chunks = std::min((1024 + tiles * H - 1) / (tiles * H), (maxL + 511) / 512);
+    d.items = score_blocks(N, maxL, B, 64 * d.key_waves, d.per_seq) * H;
+    // (one sequence may have all the rows, and a row may be listed twice)
+    const long long tiles = score_blocks(cap * G, cap * G, B, kLseRows, d.lse_per_seq);
+    long long chunks =
+        std::min((1024 + tiles * H - 1) / std::max(1LL, tiles * H), (maxL + 511) / 512);
     chunks = std::min(chunks, 64LL);
     const long long kc = ((maxL + chunks - 1) / chunks + 63) / 64 * 64;
     d.lse_kc = (int)std::min(kc, (1LL << 31) - 64);
@@ -1908,6 +1921,8 @@ logo_status logo_cache_score(const logo_problem *p, const logo_bf16 *q, const lo
     a.lse_kc = d.lse_kc;
     a.lse_chunks = d.lse_chunks;
     a.lse_items = (int32_t)d.lse_items;
+    a.per_seq = d.per_seq;
+    a.lse_per_seq = d.lse_per_seq;
     hipStream_t s = (hipStream_t)stream;
     return hip_status(launch_cache_score(a, s), s);
 }

@@ -278,7 +278,7 @@ hipError_t launch_decode_prefix(const PrefixArgs &a, hipStream_t s);
 constexpr int kLseRows = 128;               // flattened (rank, head) rows per workgroup
 struct ScoreArgs {
     const uint16_t *q, *k;
-    const int32_t *cu, *sel_idx, *cu_sel;    // sel_idx, cu_sel NULL: every token is a row
+    const int32_t *cu, *sel_idx, *cu_sel;    // cu_sel NULL: every token is a row
     const float *lse;                        // [Hq][cap], or NULL:
     float *lse_part;                         // (m, l) [lse_chunks][Hq][cap], to be computed
     const float *score_in;                   // [Hkv][n] or NULL (zeros)
@@ -288,6 +288,7 @@ struct ScoreArgs {
     float scale_log2;
     int32_t key_waves, items;                // waves side by side over the keys; workgroups
     int32_t lse_kc, lse_chunks, lse_items;
+    int32_t per_seq, lse_per_seq;            // key blocks / row tiles of every sequence, 0: search
 };
 hipError_t launch_cache_score(const ScoreArgs &a, hipStream_t s);
 

@@ -163,6 +163,42 @@ def test_prefix_gates_and_device_threshold(pk):
     check_prefix(c, x, cp, cg, cu, 64, math.inf, None, "NaN threshold")
 
 
+def test_prefix_rows_outside_the_window_are_not_read(pk):
+    """NaN in an unselected sequence's own rows before its window, and in
+    prefix keys that no query sees."""
+    import torch
+    x, cp, cg, cu = prefix_case(903, (300,), (3,), (150, 100, 70), 8, 2, 128, "")
+    x["gate"] = np.array([0.1, 0.2, 0.3], np.float32)
+    (want, _, _), args, kw = prefix_call(pk, x, cp, cg, cu, 64, 0.5)
+    prob, pre, q, kp, vp, k, v, gate = args
+    for t in (k, v):
+        for b in range(3):
+            t[cu[b]:cu[b + 1] - 64] = float("nan")
+    for t in (kp, vp):
+        t[:] = float("nan")                      # every sequence has its window in its own rows
+    got = pk.logo_decode_prefix(*args, **kw)[0]
+    torch.cuda.synchronize()
+    assert torch.equal(got.view(torch.int16), want.view(torch.int16))
+
+
+def test_two_streams(pk):
+    """Steps on two streams with workspaces of their own, interleaved."""
+    import torch
+    cases = [prefix_case(904 + i, (600 + 50 * i,), (4,), (5, 90, 30, 1), 8, 2, 128, "") for i in range(2)]
+    calls = [prefix_call(pk, *c, 128, 0.4) for c in cases]
+    torch.cuda.synchronize()
+    want = [c[0][0].clone() for c in calls]
+    streams = [torch.cuda.Stream() for _ in calls]
+    outs = []
+    for _ in range(20):
+        for (_, args, kw), s in zip(calls, streams):
+            with torch.cuda.stream(s):
+                outs.append(pk.logo_decode_prefix(*args, **kw)[0])
+    torch.cuda.synchronize()
+    for i, o in enumerate(outs):
+        assert torch.equal(o.view(torch.int16), want[i % 2].view(torch.int16)), i
+
+
 def test_prefix_without_any_rows(pk):
     """Without host copies a sequence with no rows at all outputs zeros."""
     import torch
@@ -352,6 +388,108 @@ def test_decode_score(pk, ci):
     assert torch.equal(inplace, got)
 
 
+def test_cache_score_nothing_selected(pk):
+    """No row: the scores stay as they were."""
+    import torch
+    q, k, cu, rng = score_case(80, (70, 0, 9), 4, 2, 64)
+    before = rng.random((2, 79)).astype(np.float32)
+    dev = to_device(dict(q=q, k=k, cu=cu, before=before))
+    prob = pk.Problem(dev["cu"], 4, 2, 64, 64, cu_seqlens_host=cu)
+    none = dict(sel_idx=torch.empty(0, dtype=torch.int32, device="cuda"),
+                cu_sel=torch.zeros(4, dtype=torch.int32, device="cuda"))
+    for lse in (None, torch.empty((4, 0), device="cuda")):
+        got = pk.logo_cache_score(prob, dev["q"], dev["k"], lse=lse, score_in=dev["before"], **none)
+        assert torch.equal(got, dev["before"])
+    # room for rows, but none of them selected
+    none["sel_idx"] = torch.full((50,), 1 << 30, dtype=torch.int32, device="cuda")
+    got = pk.logo_cache_score(prob, dev["q"], dev["k"], **none)
+    assert bool((got == 0).all())
+
+
+@pytest.mark.parametrize("lens", [tuple([5] * 300), tuple([3] * 150 + [2000, 0] + [1] * 149)],
+                         ids=["even", "one-long"])
+def test_cache_score_many_sequences(pk, lens):
+    """Workgroups find their sequence by a division (even lengths) or a search."""
+    q, k, cu, rng = score_case(81, lens, 2, 1, 64)
+    rows = [np.sort(rng.choice(T, (T + 2) // 3 if T < 100 else 60, replace=False)) if T else
+            np.zeros(0, np.int64) for T in lens]
+    n = [len(r) for r in rows]
+    sel = np.concatenate([r + c for r, c in zip(rows, cu)]).astype(np.int32)
+    total, size = ref.scores_of(q, k, sel, cu, n)
+    dev = to_device(dict(q=q, k=k, cu=cu, sel=sel, cu_sel=cu_of(n)))
+    prob = pk.Problem(dev["cu"], 2, 1, 64, 64, cu_seqlens_host=cu)
+    got = pk.logo_cache_score(prob, dev["q"], dev["k"], sel_idx=dev["sel"], cu_sel=dev["cu_sel"])
+    e = np.abs(got.cpu().numpy().astype(np.float64) - total)
+    assert np.all(e <= ref.score_tolerance(total, max(n) * 2, 64, size))
+
+
+def test_cache_score_row_listed_twice(pk):
+    """A row in the list twice gives its weights twice."""
+    q, k, cu, _ = score_case(82, (40, 30), 8, 2, 128)
+    sel = np.array([3, 3, 3, 17, 39, 40, 40, 69], np.int32)
+    dev = to_device(dict(q=q, k=k, cu=cu, sel=sel, cu_sel=np.array([0, 5, 8], np.int32)))
+    prob = pk.Problem(dev["cu"], 8, 2, 128, 64, cu_seqlens_host=cu)
+    total, size = ref.scores_of(q, k, sel, cu, [5, 3])
+    got = pk.logo_cache_score(prob, dev["q"], dev["k"], sel_idx=dev["sel"], cu_sel=dev["cu_sel"])
+    e = np.abs(got.cpu().numpy().astype(np.float64) - total)
+    assert np.all(e <= ref.score_tolerance(total, 5 * 4, 128, size))
+
+
+def test_offsets_past_32_bits(pk):
+    """Caches of more than 4 GiB: the second sequence lies behind the first
+    one's 2.2 million rows, and a prefix behind another one's."""
+    import torch
+    hq, hkv, d, far, L = 16, 8, 128, 2200000, 300
+    rng = np.random.default_rng(83)
+    q, k, v = bf16(rng, 1, hq, d, std=2.0), bf16(rng, L, hkv, d), bf16(rng, L, hkv, d)
+    dev = to_device(dict(q=q, k=k, v=v))
+    big_k, big_v = (torch.zeros((far + L, hkv, d), dtype=torch.bfloat16, device="cuda")
+                    for _ in range(2))
+    assert big_k.numel() * 2 > 1 << 32
+    big_k[far:], big_v[far:] = dev["k"], dev["v"]
+    cu = np.array([0, far, far + L], np.int32)
+    dcu = torch.from_numpy(cu).cuda()
+    prob = pk.Problem(dcu, hq, hkv, d, 64, cu_seqlens_host=cu)
+    want, size = ref.step_scores(q, k, [0, L], [True])
+    tol = ref.score_tolerance(want, hq // hkv, d, size)
+    # one decoding step of the second sequence
+    q2 = torch.cat([dev["q"], dev["q"]])
+    gate = torch.tensor([0.0, 1.0], device="cuda")
+    got = pk.logo_decode_score(prob, q2, big_k, gate, threshold=0.5)
+    assert bool((got[:, :far] == 0).all())
+    assert np.all(np.abs(got[:, far:].cpu().numpy() - want) <= tol)
+    # its last row as a prompt's only query
+    qq = torch.zeros((far + L, hq, d), dtype=torch.bfloat16, device="cuda")
+    qq[-1] = dev["q"][0]
+    got = pk.logo_cache_score(prob, qq, big_k,
+                              sel_idx=torch.tensor([far + L - 1], dtype=torch.int32, device="cuda"),
+                              cu_sel=torch.tensor([0, 0, 1], dtype=torch.int32, device="cuda"))
+    assert bool((got[:, :far] == 0).all())
+    assert np.all(np.abs(got[:, far:].cpu().numpy() - want) <= tol)
+    del qq, q2
+    # eviction: all scores equal in the first sequence, so its oldest rows stay
+    sc = torch.rand((hkv, far + L), device="cuda")
+    sc[:, :far] = 0.25
+    r = pk.logo_cache_evict(prob, sc, 100, recent=10, k=big_k, v=big_v)
+    kept, _ = ref.evict(sc[:, far:].cpu().numpy(), np.array([0, L]), 100, 10)
+    idx = r["keep_idx"].cpu().numpy()
+    first = list(range(90)) + list(range(far - 10, far))
+    assert (idx[:, :100] == first).all() and np.array_equal(idx[:, 100:], kept + far)
+    for h in range(hkv):
+        assert torch.equal(r["k_out"][100:, h], big_k[r["keep_idx"][h, 100:].long(), h])
+        assert torch.equal(r["v_out"][100:, h], big_v[r["keep_idx"][h, 100:].long(), h])
+    # the far rows as a shared prefix
+    own = dict(k=bf16(rng, 5, hkv, d), v=bf16(rng, 5, hkv, d), gate=np.array([0.9, 0.2], np.float32))
+    x = dict(q=np.concatenate([q, q[:, ::-1]]), k_pre=k, v_pre=v, **own)
+    cu_own, cu_grp = np.array([0, 2, 5], np.int32), np.array([0, 0, 2], np.int32)
+    d2 = to_device(dict(q=x["q"], cu=cu_own, grp=cu_grp, **own))
+    pre = pk.Prefix(dcu, d2["grp"], cu_prefix_host=cu, cu_group_host=cu_grp)
+    p2 = pk.Problem(d2["cu"], hq, hkv, d, 64, cu_seqlens_host=cu_own)
+    out = pk.logo_decode_prefix(p2, pre, d2["q"], big_k, big_v, d2["k"], d2["v"], d2["gate"],
+                                threshold=0.5)[0]
+    check_prefix(out, x, np.array([0, L]), np.array([0, 2]), cu_own, 64, 0.5, None, "far")
+
+
 # --- eviction -------------------------------------------------------------------
 def evict_scores(rng, hkv, N, kind):
     s = np.exp(2 * rng.standard_normal((hkv, N))).astype(np.float32)
@@ -421,6 +559,16 @@ def test_evict(pk, ci):
     c = pk.logo_cache_evict(bare, dev["score"], budget, recent=recent)
     torch.cuda.synchronize()
     assert c["k_out"] is None and np.array_equal(c["keep_idx"].cpu().numpy()[:, :n], kept)
+
+
+def test_evict_nothing(pk):
+    """Caches without rows, with and without outputs' room."""
+    import torch
+    cu = torch.zeros(4, dtype=torch.int32, device="cuda")
+    prob = pk.Problem(cu, 4, 2, 64, 64, cu_seqlens_host=[0, 0, 0, 0])
+    empty = torch.empty((0, 2, 64), dtype=torch.bfloat16, device="cuda")
+    r = pk.logo_cache_evict(prob, torch.empty((2, 0), device="cuda"), 5, recent=2, k=empty, v=empty)
+    assert r["cu_keep"].tolist() == [0, 0, 0, 0] and r["k_out"].shape[0] == 0
 
 
 # --- together -------------------------------------------------------------------
