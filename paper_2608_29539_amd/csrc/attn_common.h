@@ -31,12 +31,6 @@ __device__ __forceinline__ float pair_sum(float x) {
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// The larger of two: the middle of them and +inf (fmaxf makes the compiler
-// quiet its operands first, an instruction each).
-__device__ __forceinline__ float max2(float a, float b) {
-    return __builtin_amdgcn_fmed3f(a, b, __builtin_inff());
-}
-
 // Wave-uniform value, made explicit so the compiler keeps it in SGPRs.
 __device__ __forceinline__ int uni(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
@@ -96,28 +90,10 @@ __device__ __forceinline__ void lds_load4_at(u32x4 r, uint32_t lds, int voffset)
         : "memory");
 }
 
-// One 16-byte-per-lane load from a lane's own address to LDS (lane i writes
-// the 16 bytes at lds + 16 i); see lds_load16_at.
-__device__ __forceinline__ void lds_gather16(const void *src, uint32_t lds) {
-    const uint32_t lds_addr = __builtin_amdgcn_readfirstlane(lds);
-    uint32_t saved;
-    asm volatile(
-        "s_mov_b32 %0, m0\n\t"
-        "s_mov_b32 m0, %1\n\t"
-        "s_nop 0\n\t"
-        "global_load_lds_dwordx4 %2, off\n\t"
-        "s_mov_b32 m0, %0"
-        : "=&s"(saved)
-        : "s"(lds_addr), "v"(src)
-        : "memory");
-}
-
 // s_waitcnt operand that waits for vmcnt = 0 only (lgkmcnt and expcnt at
 // their maximum).  Issued through the builtin so the compiler knows that no
 // vector-memory load is outstanding afterwards.
 constexpr int kWaitVmcnt0 = 0x0F70;
-// The same for lgkmcnt (LDS reads) only.
-constexpr int kWaitLgkmcnt0 = 0xC07F;
 
 // Completion of this wave's LDS-bound loads, then the workgroup barrier.
 __device__ __forceinline__ void dma_wait_barrier() {

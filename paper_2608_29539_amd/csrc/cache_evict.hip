@@ -18,7 +18,7 @@
 //                        counts of the parts before it added up
 //   evict_copy_kernel    copies the kept rows of K and V
 #include "attn_common.h"
-#include "logo_internal.h"
+#include "cache_internal.h"
 
 namespace logo {
 namespace {

@@ -16,7 +16,8 @@
 //   step_logits_kernel      one query per sequence: the scaled scores of a
 //                           chunk of keys and their (m, l) per head
 //   step_weights_kernel     2^(score - lse) summed over the heads
-#include "attn_tiles.h"
+#include "cache_internal.h"
+#include "cache_tiles.h"
 #include "decode_common.h"
 #include "logo_internal.h"
 
@@ -83,7 +84,7 @@ __device__ __forceinline__ int token_of(const ScoreArgs &a, int rank) {
 // ---------------------------------------------------------------------------
 template <int D>
 __global__ __launch_bounds__(kScoreThreads, 2) void score_lse_kernel(const ScoreArgs a) {
-    __shared__ __attribute__((aligned(16))) uint16_t s_k[kLseBuffers][kBlockN][D + kKPad];
+    __shared__ __attribute__((aligned(16))) uint16_t s_k[kLseBuffers][kBlockN][D];
     const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6);
     const int g = lane >> 5, m = lane & 31;
     const int G = a.group;
@@ -119,22 +120,42 @@ __global__ __launch_bounds__(kScoreThreads, 2) void score_lse_kernel(const Score
     for (int s = 0; s < D / 16; s++)
         qf[s] = *(const bf16x8 *)(qp + s * 16);
 
-    // K tiles of 64 keys in four buffers, loaded three tiles ahead.  (A wave
-    // issues kPerWaveK or one less loads per tile; counting the smaller number
-    // as pending waits for no less than is needed.)
+    // K tiles of 64 keys in four buffers, loaded in order three tiles ahead: a
+    // wave's kLoads loads of each, whose addresses move on by one tile.  Keys
+    // past k1 have the last one's row (they are masked).
     constexpr int kAhead = kLseBuffers - 1;
-    constexpr int kLoads = Dma<D, kScoreWaves>::kInstK / kScoreWaves;
-    const int row_bytes = a.hkv * D * 2;
-    const uint16_t *kb = a.k + (base * a.hkv + kvh) * (int64_t)D;
-    Dma<D, kScoreWaves> dma;
-    dma_plan<D, kScoreWaves>(dma, wave, lane, row_bytes);
+    constexpr int kPc = D / 8, kLoads = kBlockN * kPc / 64 / kScoreWaves;
+    const int64_t stride = (int64_t)a.hkv * D;
+    const uint16_t *kp[kLoads];
+    int row_of[kLoads];
+#pragma unroll
+    for (int i = 0; i < kLoads; i++) {
+        const int row = ((i * kScoreWaves + wave) * 64 + lane) / kPc;
+        row_of[i] = row;
+        kp[i] = a.k + (base + k0 + row) * stride + kvh * D +
+                ((lane % kPc) ^ piece_swz<D>(row)) * 8;
+    }
     auto stage = [&](int key, int buf) {
-        if (key < k1)
-            dma_k<D, kScoreWaves>(&s_k[buf][0][0], dma, kb, k1, key, row_bytes, wave);
+        if (key >= k1)
+            return;
+        const uint32_t dst = lds_addr_of(&s_k[buf][0][0]);
+#pragma unroll
+        for (int i = 0; i < kLoads; i++) {
+            int64_t back = 0;
+            if (key + kBlockN > k1)
+                back = max(key + row_of[i] - (k1 - 1), 0) * stride;
+            lds_gather16(kp[i] - back, dst + (i * kScoreWaves + wave) * 1024);
+            kp[i] += kBlockN * stride;
+        }
     };
 #pragma unroll
     for (int i = 0; i < kAhead; i++)
         stage(k0 + i * kBlockN, i);
+    // (the queries are waited for here: a wait inside the loop would be for
+    // the tiles behind the current one too)
+#pragma unroll
+    for (int s = 0; s < D / 16; s++)
+        asm volatile("" : "+v"(qf[s]));
     const bool live = wave * 32 < nrows;
     float mr = kNegInf, l = 0.f;
     int buf = 0;
@@ -152,7 +173,8 @@ __global__ __launch_bounds__(kScoreThreads, 2) void score_lse_kernel(const Score
         for (int sb = 0; sb < 2; sb++)
 #pragma unroll
             for (int ss = 0; ss < D / 16; ss++)
-                kf[sb][ss] = *(const bf16x8 *)&s_k[buf][sb * 32 + m][ss * 16 + g * 8];
+                kf[sb][ss] = *(const bf16x8 *)&s_k[buf][sb * 32 + m]
+                                                    [((ss * 2 + g) ^ piece_swz<D>(m)) * 8];
         __builtin_amdgcn_sched_barrier(0);
         f32x16 s[2] = {};
 #pragma unroll

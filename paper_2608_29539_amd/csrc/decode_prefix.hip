@@ -25,7 +25,8 @@
 //
 // P is rounded to bf16 for the PV product, as in the layer's kernels (its row
 // sum takes the rounded values); everything else is fp32.
-#include "attn_tiles.h"
+#include "cache_internal.h"
+#include "cache_tiles.h"
 #include "decode_common.h"
 #include "logo_internal.h"
 
@@ -92,7 +93,7 @@ constexpr int kPfStages = 4;
 template <int D>
 struct alignas(16) PrefixSmem {
     uint16_t k[kPfStages][kPfKeys][D];           // pieces permuted (piece_swz)
-    uint16_t v[kPfStages][kPfKeys][D];           // segments permuted (vswz)
+    uint16_t v[kPfStages][kPfKeys][D];           // segments permuted (seg_swz)
 };
 
 template <int D>
@@ -168,7 +169,7 @@ __global__ __launch_bounds__(kPrefixThreads, 2) void prefix_attn_kernel(const Pr
         row_of[i] = row;
         const int64_t at = (k0 + row) * stride;
         kp[i] = kt + at + (c16 ^ piece_swz<D>(row)) * 8;
-        vp[i] = vt + at + (((c16 >> 2) ^ vswz<D>(row)) * 4 + (c16 & 3)) * 8;
+        vp[i] = vt + at + (((c16 >> 2) ^ seg_swz<D>(row)) * 4 + (c16 & 3)) * 8;
     }
     auto stage = [&](int buf, int key) {
         const uint32_t kd = lds_addr_of(&sm.k[buf][0][0]), vd = lds_addr_of(&sm.v[buf][0][0]);
@@ -307,7 +308,7 @@ __global__ __launch_bounds__(kPrefixThreads, 2) void prefix_attn_kernel(const Pr
                 if (!whole)
                     at -= max(key + row - (k1 - 1), 0) * stride;
                 lds_gather16(kr + at + (c16 ^ piece_swz<D>(row)) * 8, kd + ld * 1024);
-                lds_gather16(vr + at + (((c16 >> 2) ^ vswz<D>(row)) * 4 + (c16 & 3)) * 8,
+                lds_gather16(vr + at + (((c16 >> 2) ^ seg_swz<D>(row)) * 4 + (c16 & 3)) * 8,
                              vd + ld * 1024);
             }
         };
@@ -327,7 +328,7 @@ __global__ __launch_bounds__(kPrefixThreads, 2) void prefix_attn_kernel(const Pr
                 }
 #pragma unroll
             for (int x = 0; x < D / 16; x++) {
-                const uint16_t *vr = &sm.v[wave][vt_row][((x / 2) ^ vswz<D>(vt_row)) * 32 +
+                const uint16_t *vr = &sm.v[wave][vt_row][((x / 2) ^ seg_swz<D>(vt_row)) * 32 +
                                                          (x % 2) * 16 + vt_col];
                 vf[x] = lds_tr_pair(vr, vr + 16 * D);
             }
@@ -426,7 +427,7 @@ __global__ __launch_bounds__(kPrefixThreads, 2) void prefix_attn_kernel(const Pr
     int vt_scol[D / 32];
 #pragma unroll
     for (int cb = 0; cb < D / 32; cb++)
-        vt_scol[cb] = (cb ^ vswz<D>(vt_row)) * 32 + vt_col;
+        vt_scol[cb] = (cb ^ seg_swz<D>(vt_row)) * 32 + vt_col;
     f32x16 acc[D / 32];
 #pragma unroll
     for (int cb = 0; cb < D / 32; cb++)
@@ -441,7 +442,8 @@ __global__ __launch_bounds__(kPrefixThreads, 2) void prefix_attn_kernel(const Pr
     auto v_frags = [&](int buf, int ss, bf16x8 (&vf)[D / 32]) {
 #pragma unroll
         for (int cb = 0; cb < D / 32; cb++)
-            vf[cb] = read_vt_frag(&sm.v[buf][ss * 16 + vt_row][vt_scol[cb]], D);
+            vf[cb] = lds_tr_pair(&sm.v[buf][ss * 16 + vt_row][vt_scol[cb]],
+                                 &sm.v[buf][ss * 16 + vt_row + 8][vt_scol[cb]]);
     };
     auto scores = [&](f32x16 s, int ss0, const bf16x8 (&kf)[kHalf]) {
 #pragma unroll

@@ -6,6 +6,7 @@
 // stream after each launch to localise device faults).
 #include "../../include/logo.h"
 #include "logo_internal.h"
+#include "cache_internal.h"
 
 #include <algorithm>
 #include <cmath>
