@@ -120,33 +120,27 @@ __global__ __launch_bounds__(kScoreThreads, 2) void score_lse_kernel(const Score
     for (int s = 0; s < D / 16; s++)
         qf[s] = *(const bf16x8 *)(qp + s * 16);
 
-    // K tiles of 64 keys in four buffers, loaded in order three tiles ahead: a
-    // wave's kLoads loads of each, whose addresses move on by one tile.  Keys
-    // past k1 have the last one's row (they are masked).
+    // K tiles of 64 keys in four buffers, loaded three tiles ahead: kLoads loads
+    // of a wave each; rows at or past k1 read as zeros (they are masked).
     constexpr int kAhead = kLseBuffers - 1;
     constexpr int kPc = D / 8, kLoads = kBlockN * kPc / 64 / kScoreWaves;
-    const int64_t stride = (int64_t)a.hkv * D;
-    const uint16_t *kp[kLoads];
-    int row_of[kLoads];
+    const int row_bytes = a.hkv * D * 2;
+    const uint16_t *kt = a.k + (base * a.hkv + kvh) * (int64_t)D;
+    int koff[kLoads];
 #pragma unroll
     for (int i = 0; i < kLoads; i++) {
         const int row = ((i * kScoreWaves + wave) * 64 + lane) / kPc;
-        row_of[i] = row;
-        kp[i] = a.k + (base + k0 + row) * stride + kvh * D +
-                ((lane % kPc) ^ piece_swz<D>(row)) * 8;
+        koff[i] = row * row_bytes + ((lane % kPc) ^ piece_swz<D>(row)) * 16;
     }
     auto stage = [&](int key, int buf) {
         if (key >= k1)
             return;
         const uint32_t dst = lds_addr_of(&s_k[buf][0][0]);
+        const u32x4 r = raw_rsrc((const char *)kt + (int64_t)key * row_bytes,
+                                 min(kBlockN, k1 - key) * row_bytes);
 #pragma unroll
-        for (int i = 0; i < kLoads; i++) {
-            int64_t back = 0;
-            if (key + kBlockN > k1)
-                back = max(key + row_of[i] - (k1 - 1), 0) * stride;
-            lds_gather16(kp[i] - back, dst + (i * kScoreWaves + wave) * 1024);
-            kp[i] += kBlockN * stride;
-        }
+        for (int i = 0; i < kLoads; i++)
+            lds_load16_at(r, dst + (i * kScoreWaves + wave) * 1024, koff[i]);
     };
 #pragma unroll
     for (int i = 0; i < kAhead; i++)
@@ -514,18 +508,24 @@ __global__ __launch_bounds__(kStepWaves * 64) void step_logits_kernel(const Step
     // this wave's keys: its share of the chunk's blocks of 64
     const int blocks = (k1 - k0 + 63) / 64, per = (blocks + kStepWaves - 1) / kStepWaves;
     const int w0 = k0 + wave * per * 64, w1 = min(k1, w0 + per * 64);
-    const uint16_t *kb = a.k + ((int64_t)base * a.hkv + kvh) * D;
-    const int64_t stride = (int64_t)a.hkv * D;
-    // slot i of the wave: keys w0 + 16 i .. + 15; past the last key its row again
+    const char *kt = (const char *)(a.k + ((int64_t)base * a.hkv + kvh) * D);
+    const int row_bytes = a.hkv * D * 2;
+    // slot i of the wave: keys w0 + 16 i .. + 15; rows past the last key read as
+    // zeros
     const int slots = w1 > w0 ? ((w1 - w0 + 63) / 64) * 4 : 0;
+    int koff[kLoads];
+#pragma unroll
+    for (int x = 0; x < kLoads; x++) {
+        const int row = (x * 64 + lane) / kPc;
+        koff[x] = row * row_bytes + ((lane % kPc) ^ piece_swz<D>(row)) * 16;
+    }
     auto stage = [&](int i) {
         const uint32_t dst = lds_addr_of(&s_k[wave][i % kRing][0]);
+        const int key = w0 + i * 16;
+        const u32x4 r = raw_rsrc(kt + (int64_t)key * row_bytes, max(min(16, w1 - key), 0) * row_bytes);
 #pragma unroll
-        for (int x = 0; x < kLoads; x++) {
-            const int row = x * (16 / kLoads) + lane / kPc;
-            const int key = min(w0 + i * 16 + row, w1 - 1);
-            lds_gather16(kb + key * stride + ((lane % kPc) ^ piece_swz<D>(row)) * 8, dst + x * 1024);
-        }
+        for (int x = 0; x < kLoads; x++)
+            lds_load16_at(r, dst + x * 1024, koff[x]);
     };
     const int nh = min(4 * P, G - hb * 4 * P), h0 = kvh * G + hb * 4 * P;
     bf16x8 qf[D / 32];
@@ -585,13 +585,15 @@ __global__ __launch_bounds__(kStepWaves * 64) void step_logits_kernel(const Step
 #pragma unroll
         for (int x = 0; x < P; x++) {
             const int key = w0 + s0 * 16 + (x * kCopies + kg / P) * 16 + n;
-            // (the lanes past the last key or head have its score and store
-            // it again: the number of stores is what the waits count on)
-            float *lp = a.logits + base + min(key, w1 - 1);
+            // (lanes past the last key store to the room behind the scores, past
+            // the last head its score again: the number of stores is what the
+            // waits count on)
+            float *lp = a.logits + (key < w1 ? base + key : a.n * a.hq);
+            const int64_t hs = key < w1 ? a.n : 0;
 #pragma unroll
             for (int i = 0; i < 4; i++) {
                 const float v = own[x][i] * a.scale_log2;
-                lp[(int64_t)(h0 + min(4 * (kg % P) + i, nh - 1)) * a.n] = v;
+                lp[(h0 + min(4 * (kg % P) + i, nh - 1)) * hs] = v;
                 const float y = key < w1 ? v : kNegInf;
                 const float mn = fmaxf(mr[i], y), mc = mn == kNegInf ? 0.f : mn;
                 l[i] = fmaf(l[i], __builtin_amdgcn_exp2f(mr[i] - mc), __builtin_amdgcn_exp2f(y - mc));

@@ -156,33 +156,36 @@ __global__ __launch_bounds__(kPrefixThreads, 2) void prefix_attn_kernel(const Pr
     constexpr int kPc = D / 8, kLoads = kPfKeys * kPc / 64 / kPfWaves;
     const uint16_t *kt = own ? (global ? a.k_g : a.k) : (global ? a.kp_g : a.kp);
     const uint16_t *vt = own ? (global ? a.v_g : a.v) : (global ? a.vp_g : a.vp);
-    const int64_t stride = (int64_t)a.hkv * D;
-    kt += base * stride + kvh * D;
-    vt += base * stride + kvh * D;
-    // Tiles are loaded in order, so the lanes' addresses move on by one tile;
-    // keys past k1 have the last one's row (they are masked).
-    const uint16_t *kp[kLoads], *vp[kLoads];
-    int row_of[kLoads];
+    const int row_bytes = a.hkv * D * 2;
+    kt += (base * a.hkv + kvh) * (int64_t)D;
+    vt += (base * a.hkv + kvh) * (int64_t)D;
+    // A lane's byte offset inside a tile for the 1 KB of LDS that load ld fills;
+    // rows at or past k1 read as zeros (they are masked).
+    auto k_off = [&](int ld) {
+        const int row = (ld * 64 + lane) / kPc;
+        return row * row_bytes + ((lane % kPc) ^ piece_swz<D>(row)) * 16;
+    };
+    auto v_off = [&](int ld) {
+        const int row = (ld * 64 + lane) / kPc, c16 = lane % kPc;
+        return row * row_bytes + (((c16 >> 2) ^ seg_swz<D>(row)) * 4 + (c16 & 3)) * 16;
+    };
+    auto tile_at = [&](const uint16_t *t, int key) {
+        return raw_rsrc((const char *)t + (int64_t)key * row_bytes, min(kPfKeys, k1 - key) * row_bytes);
+    };
+    int koff[kLoads], voff[kLoads];
 #pragma unroll
     for (int i = 0; i < kLoads; i++) {
-        const int row = ((i * kPfWaves + wave) * 64 + lane) / kPc, c16 = lane % kPc;
-        row_of[i] = row;
-        const int64_t at = (k0 + row) * stride;
-        kp[i] = kt + at + (c16 ^ piece_swz<D>(row)) * 8;
-        vp[i] = vt + at + (((c16 >> 2) ^ seg_swz<D>(row)) * 4 + (c16 & 3)) * 8;
+        koff[i] = k_off(i * kPfWaves + wave);
+        voff[i] = v_off(i * kPfWaves + wave);
     }
     auto stage = [&](int buf, int key) {
         const uint32_t kd = lds_addr_of(&sm.k[buf][0][0]), vd = lds_addr_of(&sm.v[buf][0][0]);
+        const u32x4 kr = tile_at(kt, key), vr = tile_at(vt, key);
 #pragma unroll
         for (int i = 0; i < kLoads; i++) {
-            const int ld = i * kPfWaves + wave;
-            int64_t back = 0;
-            if (key + kPfKeys > k1)
-                back = max(key + row_of[i] - (k1 - 1), 0) * stride;
-            lds_gather16(kp[i] - back, kd + ld * 1024);
-            lds_gather16(vp[i] - back, vd + ld * 1024);
-            kp[i] += kPfKeys * stride;
-            vp[i] += kPfKeys * stride;
+            const int at = (i * kPfWaves + wave) * 1024;
+            lds_load16_at(kr, kd + at, koff[i]);
+            lds_load16_at(vr, vd + at, voff[i]);
         }
     };
     auto fill = [&]() {
@@ -295,21 +298,13 @@ __global__ __launch_bounds__(kPrefixThreads, 2) void prefix_attn_kernel(const Pr
         for (int x = 0; x < D / 16; x++)
             acc[x] = f32x4{};
         // the wave's whole tile at `key`
-        constexpr int kRowsPer = 64 / kPc;       // rows per load
         const uint32_t kd = lds_addr_of(&sm.k[wave][0][0]), vd = lds_addr_of(&sm.v[wave][0][0]);
         auto stage_own = [&](int key) {
-            const int row0 = lane / kPc, c16 = lane % kPc;
-            const uint16_t *kr = kt + (key + row0) * stride, *vr = vt + (key + row0) * stride;
-            const bool whole = key + kPfKeys <= k1;
+            const u32x4 kr = tile_at(kt, key), vr = tile_at(vt, key);
 #pragma unroll
-            for (int ld = 0; ld < kPfKeys / kRowsPer; ld++) {
-                const int row = ld * kRowsPer + row0;
-                int64_t at = (int64_t)ld * kRowsPer * stride;
-                if (!whole)
-                    at -= max(key + row - (k1 - 1), 0) * stride;
-                lds_gather16(kr + at + (c16 ^ piece_swz<D>(row)) * 8, kd + ld * 1024);
-                lds_gather16(vr + at + (((c16 >> 2) ^ seg_swz<D>(row)) * 4 + (c16 & 3)) * 8,
-                             vd + ld * 1024);
+            for (int ld = 0; ld < kPfKeys * kPc / 64; ld++) {
+                lds_load16_at(kr, kd + ld * 1024, k_off(ld));
+                lds_load16_at(vr, vd + ld * 1024, v_off(ld));
             }
         };
         dma_wait_barrier();                      // the first four tiles, the queries

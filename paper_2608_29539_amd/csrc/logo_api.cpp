@@ -460,9 +460,8 @@ ScorePlan score_plan(const logo_problem *p, int32_t cap) {
     d.items = score_blocks(N, maxL, B, 64 * d.key_waves, d.per_seq) * H;
     // (one sequence may have all the rows, and a row may be listed twice)
     const long long tiles = score_blocks(cap * G, cap * G, B, kLseRows, d.lse_per_seq);
-    long long chunks =
-        std::min((1024 + tiles * H - 1) / std::max(1LL, tiles * H), (maxL + 511) / 512);
-    chunks = std::min(chunks, 64LL);
+    const long long full = ((long long)cap * G / kLseRows + B) * H;   // without the empty places
+    const long long chunks = std::min({(1024 + full - 1) / full, (maxL + 511) / 512, 64LL});
     const long long kc = ((maxL + chunks - 1) / chunks + 63) / 64 * 64;
     d.lse_kc = (int)std::min(kc, (1LL << 31) - 64);
     d.lse_chunks = (int)((maxL + d.lse_kc - 1) / d.lse_kc);
@@ -492,7 +491,8 @@ StepScorePlan step_score_plan(const logo_problem *p) {
     d.out_chunks = (int)((maxL + kStepKeys - 1) / kStepKeys);
     d.items = B * H * d.head_blocks * d.chunks;
     d.out_items = B * H * d.out_chunks;
-    d.ml = align_up(sizeof(float) * (size_t)p->num_q_heads * p->total_tokens);
+    // (one float behind the scores that nothing reads)
+    d.ml = align_up(sizeof(float) * ((size_t)p->num_q_heads * p->total_tokens + 1));
     d.total = d.ml + align_up(2 * sizeof(float) * (size_t)B * p->num_q_heads * d.chunks);
     return d;
 }
