@@ -366,6 +366,13 @@ __global__ __launch_bounds__(kScoreThreads, 2) void score_kernel(const ScoreArgs
             meta_put(1, meta_load());
         dma_wait_barrier();
     }
+    // (the keys are waited for here: a wait inside the loop would be for the
+    // next step's rows too)
+#pragma unroll
+    for (int kb = 0; kb < 2; kb++)
+#pragma unroll
+        for (int s = 0; s < D / 16; s++)
+            asm volatile("" : "+v"(kf[kb][s]));
 #pragma unroll 1
     for (int step = 0; step < steps; step++) {
         const uint16_t *q = &s_q[step & 1][0];

@@ -48,6 +48,29 @@ __device__ __forceinline__ float quad_sum(float x) {
     return pair_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
 }
 
+// Over a row of 16 lanes and over the wave, in every lane (rotations and quad
+// swaps in the vector unit).
+template <int Ctrl>
+__device__ __forceinline__ float dpp_f(float x) {
+    return __int_as_float(
+        __builtin_amdgcn_update_dpp(0, __float_as_int(x), Ctrl, 0xF, 0xF, false));
+}
+__device__ __forceinline__ float row_sum(float x) {
+    x += dpp_f<0x128>(x);   // row_ror:8
+    x += dpp_f<0x124>(x);   // row_ror:4
+    x += dpp_f<0x4E>(x);    // quad_perm [2,3,0,1]
+    x += dpp_f<0xB1>(x);    // quad_perm [1,0,3,2]
+    return x;
+}
+__device__ __forceinline__ float wave_sum(float x) { return quad_sum(row_sum(x)); }
+__device__ __forceinline__ float wave_maxf(float x) {
+    x = fmaxf(x, dpp_f<0x128>(x));
+    x = fmaxf(x, dpp_f<0x124>(x));
+    x = fmaxf(x, dpp_f<0x4E>(x));
+    x = fmaxf(x, dpp_f<0xB1>(x));
+    return quad_max(x);
+}
+
 // Largest over the wave, in every lane.
 template <int Ctrl>
 __device__ __forceinline__ int dpp_max(int x) {
@@ -610,9 +633,7 @@ __global__ __launch_bounds__(256) void prefix_combine_kernel(const PrefixArgs a)
                 lc[i] = v[1];
             }
         }
-#pragma unroll
-        for (int sh = 1; sh < 64; sh <<= 1)
-            M = fmaxf(M, __shfl_xor(M, sh, 64));
+        M = wave_maxf(M);
         const float Mc = M == kNegInf ? 0.f : M;
         lsum = 0.f;
 #pragma unroll
@@ -624,9 +645,7 @@ __global__ __launch_bounds__(256) void prefix_combine_kernel(const PrefixArgs a)
                 lsum = fmaf(wc, lc[i], lsum);
             }
         }
-#pragma unroll
-        for (int sh = 1; sh < 64; sh <<= 1)
-            lsum += __shfl_xor(lsum, sh, 64);
+        lsum = wave_sum(lsum);
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         f32x4 A = {};
@@ -641,10 +660,8 @@ __global__ __launch_bounds__(256) void prefix_combine_kernel(const PrefixArgs a)
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // w is rewritten by the next branch
 #pragma unroll
-        for (int i = 0; i < 4; i++)
-#pragma unroll
-            for (int sh = kLanes; sh < 64; sh <<= 1)
-                A[i] += __shfl_xor(A[i], sh, 64);
+        for (int i = 0; i < 4; i++)              // the wave's groups of lanes
+            A[i] = D == 128 ? pair_sum(A[i]) : quad_sum(A[i]);
         return A;
     };
     float ml = kNegInf, ll = 0.f, mg = kNegInf, lg = 0.f;
@@ -683,9 +700,9 @@ __global__ __launch_bounds__(256) void prefix_combine_kernel(const PrefixArgs a)
             o[i] *= inv;
             ss = fmaf(o[i], o[i], ss);
         }
-#pragma unroll
-        for (int sh = 1; sh < kLanes; sh <<= 1)
-            ss += __shfl_xor(ss, sh, 64);
+        ss = row_sum(ss);
+        if (D == 128)                            // (32 lanes: two rows)
+            ss += __shfl_xor(ss, 16, 64);
         const float rn = 1.f / sqrtf(ss / (float)D + a.eps);
 #pragma unroll
         for (int i = 0; i < 4; i++)
