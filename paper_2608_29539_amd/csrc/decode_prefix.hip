@@ -148,7 +148,7 @@ __global__ __launch_bounds__(kPrefixThreads, 2) void prefix_attn_kernel(const Pr
         t = rem / kQueues;
         pair = u * kQueues + rem % kQueues;
     }
-    const int pk = pair / a.hkv, kvh = pair % a.hkv, r = pk / nch, c = pk % nch;
+    const int pk = pair / nch, c = pair % nch, kvh = pk % a.hkv, r = pk / a.hkv;
     if (r >= (own ? a.num_seqs : a.num_prefixes))
         return;
     // (all of them read before the first is looked at)
