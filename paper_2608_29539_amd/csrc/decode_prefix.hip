@@ -25,6 +25,13 @@
 //
 // P is rounded to bf16 for the PV product, as in the layer's kernels (its row
 // sum takes the rounded values); everything else is fp32.
+//
+// Bounds (32 / 8 heads, d = 128).  32 sequences behind 16K tokens, 4 selected:
+// reading 171 MB, 31 us + 6.5 of merge (5.5 TB/s from the last-level cache).
+// 64 behind 32K, all selected: a wave's chain per tile (fragment reads, the
+// running max, exponentials, two products of 256 cycles), 73 us + 8 for 36
+// GFLOP; 64-key tiles and deeper or shallower prefetch took the same time.
+// Small steps: the prologue (4 us of dependent loads) and the merge's.
 #include "cache_internal.h"
 #include "cache_tiles.h"
 #include "decode_common.h"
