@@ -604,11 +604,19 @@ __global__ __launch_bounds__(256) void prefix_combine_kernel(const PrefixArgs a)
     const float p = a.gate[b];
     const bool sel = p > decode_threshold(a);
 
-    // (m, l) of one branch and its unnormalised output: this stream's part of
-    // it in A
-    auto branch = [&](int kp, int ko, float &M, float &lsum) {
-        // written chunks of the two ranges
-        int first[2], n[2];
+    // One branch's written chunks: begin() issues the loads of their (m, l) and
+    // of the stream's first kPre parts, finish() weights and adds them.
+    constexpr int kPre = 4;
+    struct Branch {
+        int first[2], n[2], total;               // slots of the two ranges
+        f32x2 ml[kMost / 64];
+        f32x4 pre[kPre];
+    };
+    auto row_of = [&](const Branch &x, int j) {
+        const int slot = j < x.n[0] ? x.first[0] + j : x.first[1] + j - x.n[0];
+        return (int64_t)slot * rows + job;
+    };
+    auto begin = [&](int kp, int ko, Branch &x) {
         const int kinds[2] = {kp, ko};
 #pragma unroll
         for (int i = 0; i < 2; i++) {
@@ -616,54 +624,54 @@ __global__ __launch_bounds__(256) void prefix_combine_kernel(const PrefixArgs a)
             int lo, hi;
             key_range(a, kind, P, S, lo, hi);
             const int base = chunk_base(a, kind, len), kc = a.kc[kind];
-            first[i] = lo < hi ? (lo - base) / kc : 0;
+            const int c0 = lo < hi ? (lo - base) / kc : 0;
             const int end = lo < hi ? min((hi - base + kc - 1) / kc, a.chunks[kind]) : 0;
-            n[i] = max(0, end - first[i]);
-            first[i] += a.slot0[kind];
+            x.n[i] = max(0, end - c0);
+            x.first[i] = a.slot0[kind] + c0;
         }
-        const int total = n[0] + n[1];
-        auto row_of = [&](int j) {
-            const int slot = j < n[0] ? first[0] + j : first[1] + j - n[0];
-            return (int64_t)slot * rows + job;
-        };
-        M = kNegInf;
-        float *w = s_w[wave];
-        float lc[kMost / 64];
+        x.total = x.n[0] + x.n[1];
 #pragma unroll
         for (int i = 0; i < kMost / 64; i++) {
             const int j = lane + 64 * i;
-            lc[i] = 0.f;
-            if (j < total) {
-                const f32x2 v = *(const f32x2 *)(a.ml + 2 * row_of(j));
-                w[j] = v[0];
-                M = fmaxf(M, v[0]);
-                lc[i] = v[1];
-            }
+            x.ml[i] = j < x.total ? *(const f32x2 *)(a.ml + 2 * row_of(x, j)) : f32x2{kNegInf, 0.f};
         }
+#pragma unroll
+        for (int u = 0; u < kPre; u++) {
+            const int j = st + u * kStreams;
+            x.pre[u] = j < x.total ? *(const f32x4 *)(a.part + row_of(x, j) * D + 4 * e) : f32x4{};
+        }
+    };
+    auto finish = [&](const Branch &x, float &M, float &lsum) {
+        M = kNegInf;
+#pragma unroll
+        for (int i = 0; i < kMost / 64; i++)
+            M = fmaxf(M, x.ml[i][0]);
         M = wave_maxf(M);
         const float Mc = M == kNegInf ? 0.f : M;
+        float *w = s_w[wave];
         lsum = 0.f;
 #pragma unroll
         for (int i = 0; i < kMost / 64; i++) {
-            const int j = lane + 64 * i;
-            if (j < total) {
-                const float wc = __builtin_amdgcn_exp2f(w[j] - Mc);
-                w[j] = wc;
-                lsum = fmaf(wc, lc[i], lsum);
-            }
+            const float wc = __builtin_amdgcn_exp2f(x.ml[i][0] - Mc);
+            w[lane + 64 * i] = wc;
+            lsum = fmaf(wc, x.ml[i][1], lsum);
         }
         lsum = wave_sum(lsum);
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         f32x4 A = {};
-#pragma unroll 4
-        for (int j = st; j < total; j += kStreams) {
-            const f32x4 v = *(const f32x4 *)(a.part + row_of(j) * D + 4 * e);
-            const float wc = w[j];
+        auto add = [&](float wc, const f32x4 v) {
 #pragma unroll
             for (int i = 0; i < 4; i++)
                 A[i] = fmaf(wc, v[i], A[i]);
-        }
+        };
+#pragma unroll
+        for (int u = 0; u < kPre; u++)           // (past the last chunk: weight and part 0)
+            if (st + u * kStreams < kMost)
+                add(w[st + u * kStreams], x.pre[u]);
+#pragma unroll 4
+        for (int j = st + kPre * kStreams; j < x.total; j += kStreams)
+            add(w[j], *(const f32x4 *)(a.part + row_of(x, j) * D + 4 * e));
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // w is rewritten by the next branch
 #pragma unroll
@@ -671,10 +679,14 @@ __global__ __launch_bounds__(256) void prefix_combine_kernel(const PrefixArgs a)
             A[i] = D == 128 ? pair_sum(A[i]) : quad_sum(A[i]);
         return A;
     };
-    float ml = kNegInf, ll = 0.f, mg = kNegInf, lg = 0.f;
-    f32x4 ol = branch(kPfxLocal, kOwnLocal, ml, ll), og = {};
+    Branch local, global;
+    begin(kPfxLocal, kOwnLocal, local);
     if (sel)                                      // (every wave of the head)
-        og = branch(kPfxGlobal, kOwnGlobal, mg, lg);
+        begin(kPfxGlobal, kOwnGlobal, global);
+    float ml = kNegInf, ll = 0.f, mg = kNegInf, lg = 0.f;
+    f32x4 ol = finish(local, ml, ll), og = {};
+    if (sel)
+        og = finish(global, mg, lg);
     if constexpr (WPH > 1) {
         if (lane < kLanes) {
             *(f32x4 *)&s_o[0][wave][4 * e] = ol;
@@ -734,7 +746,9 @@ hipError_t launch_d(const PrefixArgs &a, hipStream_t s) {
     if (e != hipSuccess)
         return e;
     const int64_t jobs = (int64_t)a.num_seqs * a.hq;
-    if (a.chunks[kPfxGlobal] + a.chunks[kOwnGlobal] > kWidePrefixMerge)
+    // four waves per head where a head has many chunks and the heads alone do
+    // not fill the card (64 sequences, 32 heads, 33 chunks: 13.1 us, 11 with one)
+    if (a.chunks[kPfxGlobal] + a.chunks[kOwnGlobal] > kWidePrefixMerge && jobs <= 1024)
         hipLaunchKernelGGL((prefix_combine_kernel<D, 4>), dim3(jobs), dim3(256), 0, s, a);
     else
         hipLaunchKernelGGL((prefix_combine_kernel<D, 1>), dim3((jobs + 3) / 4), dim3(256), 0, s, a);

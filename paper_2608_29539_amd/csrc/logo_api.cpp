@@ -386,14 +386,14 @@ struct PrefixPlan {
     size_t ml, total;
 };
 
-// Keys per chunk.  The prefix's part of the global branch: about 256
-// workgroups (one per CU, the other ranges' beside them) over the KV heads and
-// row tiles, at least 128 keys each; with 512 the step of 32 sequences behind
-// 16K tokens took 43 us instead of 38 (partial results, more starts), with 128
-// that of 64 behind 32K 126 instead of 87.  The sequences' own rows: 512 keys,
-// 256 where that makes fewer than 512 workgroups (23 sequences, 2 KV heads:
-// 32 and 24 us; 32 and 8: 38 and 39).  The window's part of a prefix: 256.
-// At most kMaxPrefixChunks each.
+// Keys per chunk.  The prefix's part of the global branch: about 320
+// workgroups over the KV heads and row tiles (one per CU and some, the other
+// ranges' beside them), at least 256 keys each: 32 sequences behind 16K tokens
+// 45.9 us (512 workgroups 49.9), 64 behind 32K 76.3 (256: 79.0, 512: 80.7, 128:
+// 122), three groups behind 17.6K in all 21.9 (384 of at least 128 keys: 25.6).
+// The sequences' own rows: 512 keys, 256 where that makes fewer than 512
+// workgroups (23 sequences, 2 KV heads: 32 and 24 us; 32 and 8: 38 and 39).
+// The window's part of a prefix: 256.  At most kMaxPrefixChunks each.
 PrefixPlan prefix_plan(const logo_problem *p, const logo_prefix *x, bool share) {
     PrefixPlan d;
     const long long G = p->num_q_heads / p->num_kv_heads, w = p->window;
@@ -406,7 +406,7 @@ PrefixPlan prefix_plan(const logo_problem *p, const logo_prefix *x, bool share) 
     const long long own_items = p->num_seqs * (long long)p->num_kv_heads * d.own_tiles *
                                 ((maxS + 511) / 512);
     const long long own = own_items >= 512 ? 512 : 256;
-    const long long want[4] = {std::max(128LL, (work + 255) / 256), own, 256, own};
+    const long long want[4] = {std::max(256LL, (work + 319) / 320), own, 256, own};
     long long slots = 0, first = 0;
     for (int i = 0; i < 4; i++) {
         long long kc = std::max(want[i], (span[i] + kMaxPrefixChunks - 1) / kMaxPrefixChunks);
@@ -2043,6 +2043,7 @@ logo_status logo_cache_evict(const logo_problem *p, const float *score, int32_t 
     a.keep_idx = keep_idx;
     a.cu_keep = cu_keep;
     a.parts = (int32_t)d.parts;
+    a.small = p->max_seqlen <= kEvSmallRows;
     a.hist = (uint32_t *)ws;
     a.picks = (uint32_t *)((char *)ws + d.picks);
     a.above = (uint32_t *)((char *)ws + d.above);
