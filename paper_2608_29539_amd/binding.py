@@ -867,7 +867,9 @@ def logo_decode_prefix(prob: Problem, prefix: Prefix, q, k_pre, v_pre, k, v, gat
     if ws is None:
         ws = torch.empty(logo_decode_prefix_workspace_bytes(prob, prefix), dtype=torch.uint8,
                          device=q.device)
-    _here(q, k, v, k_pre, v_pre, gate, out, ws, prob.cu_seqlens, prefix.cu_prefix, prefix.cu_group)
+    _here(q, k, v, k_pre, v_pre, q_g, k_g, v_g, k_pre_g, v_pre_g, gate, threshold_device,
+          gain_local, gain_global, out, active, n_active, ws, prob.cu_seqlens, prefix.cu_prefix,
+          prefix.cu_group)
     _call("logo_decode_prefix", prob.c, prefix.c, _ptr(q), _ptr(k_pre), _ptr(v_pre), _ptr(k),
           _ptr(v), _ptr(q_g), _ptr(k_pre_g), _ptr(v_pre_g), _ptr(k_g), _ptr(v_g), _ptr(gate),
           mode, float(threshold if threshold is not None else 0.0), _ptr(threshold_device),
@@ -910,7 +912,7 @@ def logo_cache_score(prob: Problem, q, k, *, sel_idx=None, cu_sel=None, lse=None
     nbytes = 0
     if lse is None:
         ws, nbytes = _ws(prob, LOGO_ENTRY_CACHE_SCORE, cap, ws)
-    _here(q, k, score, sel_idx, lse, ws, prob.cu_seqlens)
+    _here(q, k, score_in, score, sel_idx, cu_sel, lse, ws, prob.cu_seqlens)
     _call("logo_cache_score", prob.c, _ptr(q), _ptr(k), _ptr(sel_idx), _ptr(cu_sel), int(cap),
           _ptr(lse), _ptr(score_in), _ptr(score), _ptr(ws), nbytes, _stream())
     return score
@@ -930,7 +932,7 @@ def logo_decode_score(prob: Problem, q, k, gate, *, threshold: Optional[float] =
     _check(gate, torch.float32, (B,), "gate")
     score = _check_scores(prob, score_in, score, q.device)
     ws, nbytes = _ws(prob, LOGO_ENTRY_DECODE_SCORE, 0, ws)
-    _here(q, k, gate, score, ws, prob.cu_seqlens)
+    _here(q, k, gate, threshold_device, score_in, score, ws, prob.cu_seqlens)
     _call("logo_decode_score", prob.c, _ptr(q), _ptr(k), _ptr(gate), mode,
           float(threshold if threshold is not None else 0.0), _ptr(threshold_device),
           _ptr(score_in), _ptr(score), _ptr(ws), nbytes, _stream())
@@ -980,7 +982,7 @@ def logo_cache_evict(prob: Problem, score, budget: int, *, recent: int = 0, k=No
     _check(r["keep_idx"], torch.int32, (Hkv, cap), "keep_idx")
     _check(r["cu_keep"], torch.int32, (B + 1,), "cu_keep")
     ws, nbytes = _ws(prob, LOGO_ENTRY_CACHE_EVICT, 0, ws)
-    _here(score, k, k_g, r["k_out"], r["score_out"], ws, prob.cu_seqlens)
+    _here(score, k, v, k_g, v_g, ws, prob.cu_seqlens, *r.values())
     _call("logo_cache_evict", prob.c, _ptr(score), int(budget), int(recent), _ptr(k), _ptr(v),
           _ptr(k_g), _ptr(v_g), _ptr(r["k_out"]), _ptr(r["v_out"]), _ptr(r["k_g_out"]),
           _ptr(r["v_g_out"]), _ptr(r["score_out"]), _ptr(r["keep_idx"]), _ptr(r["cu_keep"]), cap,

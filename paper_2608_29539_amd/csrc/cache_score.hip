@@ -110,7 +110,7 @@ __global__ __launch_bounds__(kScoreThreads, 2) void score_lse_kernel(const Score
     const int64_t tok = token_of(a, rank);
     const int pos = (int)(tok - base);
     const int pos_end = (int)(token_of(a, s0 + (int)((r0 + nrows - 1) / G)) - base);
-    const int k0 = c * a.lse_kc, k1 = min(pos_end + 1, k0 + a.lse_kc);
+    const int k0 = c * a.lse_kc, k1 = k0 + min(pos_end + 1 - k0, a.lse_kc);
     if (k0 >= k1)
         return;
     const int pos_min = uni(pos);                // rows ascend
@@ -215,9 +215,10 @@ __global__ __launch_bounds__(kScoreThreads, 2) void score_lse_kernel(const Score
 // through LDS, kScoreRows at a time in two buffers filled by direct loads: a
 // step has the next one's rows on their way while it multiplies its own, and
 // the addresses, positions and lse of the one after that, so that a step waits
-// for no chain of loads.  A row's 16-byte pieces are permuted (piece_swz).  Each Q fragment feeds two products (the wave's two blocks of 32
-// keys), and the exponentials of one block of rows are issued between the
-// products of the next.  4096 rows on 32768 keys, 32 / 8 heads: 590 us, 930
+// for no chain of loads.  A row's 16-byte pieces are permuted (piece_swz).
+// Each Q fragment feeds two products (the wave's two blocks of 32 keys), and
+// the exponentials of one block of rows are issued between the products of the
+// next.  4096 rows on 32768 keys, 32 / 8 heads: 590 us, 930
 // TFLOP/s (1088 with rows staged through registers in 64-row steps); matrix
 // cores busy in 44% of the cycles, the vector unit in 58%, of which the
 // exponentials are half.

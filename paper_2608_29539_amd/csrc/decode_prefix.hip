@@ -27,9 +27,9 @@
 // sum takes the rounded values); everything else is fp32.
 //
 // Bounds (32 / 8 heads, d = 128).  32 sequences behind 16K tokens, 4 selected:
-// reading 171 MB, 31 us + 6.5 of merge (5.5 TB/s from the last-level cache).
+// reading 171 MB, 31 us + 5.9 of merge (5.5 TB/s from the last-level cache).
 // 64 behind 32K, all selected: a wave's chain per tile (fragment reads, the
-// running max, exponentials, two products of 256 cycles), 73 us + 8 for 36
+// running max, exponentials, two products of 256 cycles), 69 us + 7.6 for 36
 // GFLOP; 64-key tiles and deeper or shallower prefetch took the same time.
 // Small steps: the prologue (4 us of dependent loads) and the merge's.
 #include "cache_internal.h"
@@ -747,7 +747,8 @@ hipError_t launch_d(const PrefixArgs &a, hipStream_t s) {
         return e;
     const int64_t jobs = (int64_t)a.num_seqs * a.hq;
     // four waves per head where a head has many chunks and the heads alone do
-    // not fill the card (64 sequences, 32 heads, 33 chunks: 13.1 us, 11 with one)
+    // not fill the card (64 sequences of 32 heads behind 32K tokens, 2048 heads:
+    // the step 78.5 us with four, 76.7 with one)
     if (a.chunks[kPfxGlobal] + a.chunks[kOwnGlobal] > kWidePrefixMerge && jobs <= 1024)
         hipLaunchKernelGGL((prefix_combine_kernel<D, 4>), dim3(jobs), dim3(256), 0, s, a);
     else

@@ -410,7 +410,8 @@ PrefixPlan prefix_plan(const logo_problem *p, const logo_prefix *x, bool share) 
     long long slots = 0, first = 0;
     for (int i = 0; i < 4; i++) {
         long long kc = std::max(want[i], (span[i] + kMaxPrefixChunks - 1) / kMaxPrefixChunks);
-        kc = std::min((kc + kBlockN - 1) / kBlockN * kBlockN, (1LL << 31) - kBlockN);
+        // (a position and a chunk behind it stay 32-bit)
+        kc = std::min((kc + kBlockN - 1) / kBlockN * kBlockN, 1LL << 26);
         d.kc[i] = (int)kc;
         d.chunks[i] = (int)((span[i] + kc - 1) / kc);
         d.slot0[i] = (int)slots;
@@ -2043,7 +2044,6 @@ logo_status logo_cache_evict(const logo_problem *p, const float *score, int32_t 
     a.keep_idx = keep_idx;
     a.cu_keep = cu_keep;
     a.parts = (int32_t)d.parts;
-    a.small = p->max_seqlen <= kEvSmallRows;
     a.hist = (uint32_t *)ws;
     a.picks = (uint32_t *)((char *)ws + d.picks);
     a.above = (uint32_t *)((char *)ws + d.above);
