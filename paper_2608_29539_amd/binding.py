@@ -803,14 +803,27 @@ def logo_decode_noalloc(prob: Problem, q, k, v, gate, out, *, threshold: Optiona
     return out, active, n_active
 
 
-def _here(*tensors):
-    """Refuses tensors of another device than the current one, whose stream
-    the call would run on."""
+def _checks_here():
+    """``_check`` that also refuses tensors of another device than the current
+    one, whose stream the call would run on, and the same for tensors of which
+    nothing else is checked."""
     import torch
-    dev = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and t.device.index != dev:
-            raise ValueError(f"tensor on {t.device}, but the current device is {dev}")
+    dev = torch.cuda.current_device() if torch.cuda.is_initialized() else None
+
+    def here(*tensors):
+        for t in tensors:
+            if t is not None and t.get_device() != dev:
+                raise ValueError(f"tensor on {t.device}, but the current device is {dev}")
+
+    def check(t, dtype, shape, name):
+        if (t is not None and t.dtype == dtype and t.get_device() == dev and t.is_contiguous()
+                and (shape is None or t.shape == shape)):
+            return t
+        _check(t, dtype, shape, name)
+        here(t)
+        return t
+
+    return check, here
 
 
 def _step_threshold(threshold, threshold_device):
@@ -845,31 +858,30 @@ def logo_decode_prefix(prob: Problem, prefix: Prefix, q, k_pre, v_pre, k, v, gat
                         prob.num_seqs)
     P = prefix.total_tokens
     mode = _step_threshold(threshold, threshold_device)
-    _check(q, torch.bfloat16, (B, Hq, d), "q")
+    check, here = _checks_here()
+    check(q, torch.bfloat16, (B, Hq, d), "q")
     for t, nm, n in ((k_pre, "k_pre", P), (v_pre, "v_pre", P), (k, "k", N), (v, "v", N)):
-        _check(t, torch.bfloat16, (n, Hkv, d), nm)
+        check(t, torch.bfloat16, (n, Hkv, d), nm)
     for t, nm, shp in ((q_g, "q_g", (B, Hq, d)), (k_pre_g, "k_pre_g", (P, Hkv, d)),
                        (v_pre_g, "v_pre_g", (P, Hkv, d)), (k_g, "k_g", (N, Hkv, d)),
                        (v_g, "v_g", (N, Hkv, d))):
         if t is not None:
-            _check(t, torch.bfloat16, shp, nm)
+            check(t, torch.bfloat16, shp, nm)
     for t, nm in ((gain_local, "gain_local"), (gain_global, "gain_global")):
         if t is not None:
-            _check(t, torch.float32, (Hq, d), nm)
-    _check(gate, torch.float32, (B,), "gate")
+            check(t, torch.float32, (Hq, d), nm)
+    check(gate, torch.float32, (B,), "gate")
     if out is None:
         out = torch.empty((B, Hq, d), dtype=torch.bfloat16, device=q.device)
-    _check(out, torch.bfloat16, (B, Hq, d), "out")
+    check(out, torch.bfloat16, (B, Hq, d), "out")
     if active is not None:
-        _check(active, torch.int32, (B,), "active")
+        check(active, torch.int32, (B,), "active")
     if n_active is not None:
-        _check(n_active, torch.int32, (1,), "n_active")
+        check(n_active, torch.int32, (1,), "n_active")
     if ws is None:
         ws = torch.empty(logo_decode_prefix_workspace_bytes(prob, prefix), dtype=torch.uint8,
                          device=q.device)
-    _here(q, k, v, k_pre, v_pre, q_g, k_g, v_g, k_pre_g, v_pre_g, gate, threshold_device,
-          gain_local, gain_global, out, active, n_active, ws, prob.cu_seqlens, prefix.cu_prefix,
-          prefix.cu_group)
+    here(threshold_device, ws, prob.cu_seqlens, prefix.cu_prefix, prefix.cu_group)
     _call("logo_decode_prefix", prob.c, prefix.c, _ptr(q), _ptr(k_pre), _ptr(v_pre), _ptr(k),
           _ptr(v), _ptr(q_g), _ptr(k_pre_g), _ptr(v_pre_g), _ptr(k_g), _ptr(v_g), _ptr(gate),
           mode, float(threshold if threshold is not None else 0.0), _ptr(threshold_device),
@@ -878,15 +890,15 @@ def logo_decode_prefix(prob: Problem, prefix: Prefix, q, k_pre, v_pre, k, v, gat
     return out, active, n_active
 
 
-def _check_scores(prob: Problem, score_in, score, device):
+def _check_scores(check, prob: Problem, score_in, score, device):
     """score_in as given (or None) and score, allocated when not given."""
     import torch
     shape = (prob.num_kv_heads, prob.total_tokens)
     if score_in is not None:
-        _check(score_in, torch.float32, shape, "score_in")
+        check(score_in, torch.float32, shape, "score_in")
     if score is None:
         score = torch.empty(shape, dtype=torch.float32, device=device)
-    return _check(score, torch.float32, shape, "score")
+    return check(score, torch.float32, shape, "score")
 
 
 def logo_cache_score(prob: Problem, q, k, *, sel_idx=None, cu_sel=None, lse=None, score_in=None,
@@ -897,22 +909,23 @@ def logo_cache_score(prob: Problem, q, k, *, sel_idx=None, cu_sel=None, lse=None
     the forward's base-2 log-sum-exp; without it it is computed."""
     import torch
     N, Hq, Hkv, d = prob.total_tokens, prob.num_q_heads, prob.num_kv_heads, prob.head_dim
-    _check(q, torch.bfloat16, (N, Hq, d), "q")
-    _check(k, torch.bfloat16, (N, Hkv, d), "k")
+    check, here = _checks_here()
+    check(q, torch.bfloat16, (N, Hq, d), "q")
+    check(k, torch.bfloat16, (N, Hkv, d), "k")
     if (sel_idx is None) != (cu_sel is None):
         raise ValueError("give sel_idx and cu_sel together")
     cap = N
     if sel_idx is not None:
-        _check(sel_idx, torch.int32, None, "sel_idx")
-        _check(cu_sel, torch.int32, (prob.num_seqs + 1,), "cu_sel")
+        check(sel_idx, torch.int32, None, "sel_idx")
+        check(cu_sel, torch.int32, (prob.num_seqs + 1,), "cu_sel")
         cap = sel_idx.numel()
     if lse is not None:
-        _check(lse, torch.float32, (Hq, cap), "lse")
-    score = _check_scores(prob, score_in, score, q.device)
+        check(lse, torch.float32, (Hq, cap), "lse")
+    score = _check_scores(check, prob, score_in, score, q.device)
     nbytes = 0
     if lse is None:
         ws, nbytes = _ws(prob, LOGO_ENTRY_CACHE_SCORE, cap, ws)
-    _here(q, k, score_in, score, sel_idx, cu_sel, lse, ws, prob.cu_seqlens)
+    here(ws, prob.cu_seqlens)
     _call("logo_cache_score", prob.c, _ptr(q), _ptr(k), _ptr(sel_idx), _ptr(cu_sel), int(cap),
           _ptr(lse), _ptr(score_in), _ptr(score), _ptr(ws), nbytes, _stream())
     return score
@@ -927,12 +940,13 @@ def logo_decode_score(prob: Problem, q, k, gate, *, threshold: Optional[float] =
     N, Hq, Hkv, d, B = (prob.total_tokens, prob.num_q_heads, prob.num_kv_heads, prob.head_dim,
                         prob.num_seqs)
     mode = _step_threshold(threshold, threshold_device)
-    _check(q, torch.bfloat16, (B, Hq, d), "q")
-    _check(k, torch.bfloat16, (N, Hkv, d), "k")
-    _check(gate, torch.float32, (B,), "gate")
-    score = _check_scores(prob, score_in, score, q.device)
+    check, here = _checks_here()
+    check(q, torch.bfloat16, (B, Hq, d), "q")
+    check(k, torch.bfloat16, (N, Hkv, d), "k")
+    check(gate, torch.float32, (B,), "gate")
+    score = _check_scores(check, prob, score_in, score, q.device)
     ws, nbytes = _ws(prob, LOGO_ENTRY_DECODE_SCORE, 0, ws)
-    _here(q, k, gate, threshold_device, score_in, score, ws, prob.cu_seqlens)
+    here(threshold_device, ws, prob.cu_seqlens)
     _call("logo_decode_score", prob.c, _ptr(q), _ptr(k), _ptr(gate), mode,
           float(threshold if threshold is not None else 0.0), _ptr(threshold_device),
           _ptr(score_in), _ptr(score), _ptr(ws), nbytes, _stream())
@@ -953,41 +967,43 @@ def logo_cache_evict(prob: Problem, score, budget: int, *, recent: int = 0, k=No
     v_g_out (None without their inputs), score_out, keep_idx and cu_keep."""
     import torch
     N, Hkv, d, B = prob.total_tokens, prob.num_kv_heads, prob.head_dim, prob.num_seqs
-    dev = prob.cu_seqlens.device
-    _check(score, torch.float32, (Hkv, N), "score")
+    check, here = _checks_here()
+    check(score, torch.float32, (Hkv, N), "score")
     cap = None
     for t, dim in ((score_out, 1), (keep_idx, 1), (k_out, 0), (v_out, 0), (k_g_out, 0),
                    (v_g_out, 0)):
-        if t is not None and cap is None:
+        if t is not None:
             cap = int(t.shape[dim])
+            break
     if cap is None:
         cap = max(logo_cache_keep_capacity(prob, budget), 0)
-    r = dict(k_out=k_out, v_out=v_out, k_g_out=k_g_out, v_g_out=v_g_out, score_out=score_out,
-             keep_idx=keep_idx, cu_keep=cu_keep)
-    for t, nm in ((k, "k"), (v, "v"), (k_g, "k_g"), (v_g, "v_g")):
-        o = nm + "_out"
+    here(ws, prob.cu_seqlens)
+
+    def rows(t, o, nm):
         if t is not None:
-            _check(t, torch.bfloat16, (N, Hkv, d), nm)
-            if r[o] is None:
-                r[o] = torch.empty((cap, Hkv, d), dtype=torch.bfloat16, device=dev)
-        if r[o] is not None:
-            _check(r[o], torch.bfloat16, (cap, Hkv, d), o)
-    if score_out is None:
-        r["score_out"] = torch.empty((Hkv, cap), dtype=torch.float32, device=dev)
-    if keep_idx is None:
-        r["keep_idx"] = torch.empty((Hkv, cap), dtype=torch.int32, device=dev)
-    if cu_keep is None:
-        r["cu_keep"] = torch.empty(B + 1, dtype=torch.int32, device=dev)
-    _check(r["score_out"], torch.float32, (Hkv, cap), "score_out")
-    _check(r["keep_idx"], torch.int32, (Hkv, cap), "keep_idx")
-    _check(r["cu_keep"], torch.int32, (B + 1,), "cu_keep")
+            check(t, torch.bfloat16, (N, Hkv, d), nm)
+            if o is None:
+                return torch.empty((cap, Hkv, d), dtype=torch.bfloat16, device=score.device)
+        if o is not None:
+            check(o, torch.bfloat16, (cap, Hkv, d), nm + "_out")
+        return o
+
+    def given(t, dtype, shape, nm):
+        if t is None:
+            return torch.empty(shape, dtype=dtype, device=score.device)
+        return check(t, dtype, shape, nm)
+
+    k_out, v_out = rows(k, k_out, "k"), rows(v, v_out, "v")
+    k_g_out, v_g_out = rows(k_g, k_g_out, "k_g"), rows(v_g, v_g_out, "v_g")
+    score_out = given(score_out, torch.float32, (Hkv, cap), "score_out")
+    keep_idx = given(keep_idx, torch.int32, (Hkv, cap), "keep_idx")
+    cu_keep = given(cu_keep, torch.int32, (B + 1,), "cu_keep")
     ws, nbytes = _ws(prob, LOGO_ENTRY_CACHE_EVICT, 0, ws)
-    _here(score, k, v, k_g, v_g, ws, prob.cu_seqlens, *r.values())
     _call("logo_cache_evict", prob.c, _ptr(score), int(budget), int(recent), _ptr(k), _ptr(v),
-          _ptr(k_g), _ptr(v_g), _ptr(r["k_out"]), _ptr(r["v_out"]), _ptr(r["k_g_out"]),
-          _ptr(r["v_g_out"]), _ptr(r["score_out"]), _ptr(r["keep_idx"]), _ptr(r["cu_keep"]), cap,
-          _ptr(ws), nbytes, _stream())
-    return r
+          _ptr(k_g), _ptr(v_g), _ptr(k_out), _ptr(v_out), _ptr(k_g_out), _ptr(v_g_out),
+          _ptr(score_out), _ptr(keep_idx), _ptr(cu_keep), cap, _ptr(ws), nbytes, _stream())
+    return dict(k_out=k_out, v_out=v_out, k_g_out=k_g_out, v_g_out=v_g_out, score_out=score_out,
+                keep_idx=keep_idx, cu_keep=cu_keep)
 
 
 def logo_gate_proj(x, w_g, out=None):

@@ -10,7 +10,10 @@
 // get their places by counting.  A workgroup has 8192 rows in registers.
 //
 //   evict_select_kernel  caches of up to 8192 rows: one workgroup per (sequence,
-//                        KV head) does it all, with the histograms in LDS
+//                        KV head) does it all, with the histograms in LDS (up
+//                        to 2048 rows of 256 threads, whose barriers and scans
+//                        are shorter: 4 caches of 2048 rows 7.5 us, 10.1 with
+//                        1024)
 //   evict_hist_kernel    longer ones: a launch per digit, in which every part
 //                        of 8192 rows adds up all parts' last histograms, picks
 //                        the bin of the k-th and counts the next digit
@@ -27,8 +30,7 @@
 namespace logo {
 namespace {
 
-constexpr int kEvThreads = 1024;
-constexpr int kEvWaves = kEvThreads / 64;
+constexpr int kEvThreads = 1024;                           // of a part of kEvPartRows
 constexpr int kEvPer = kEvPartRows / kEvThreads;           // rows per thread
 constexpr int kEvBins = 2048;
 
@@ -58,8 +60,10 @@ __device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
 
 // What the waves exchange: sums of theirs in turn in two places, so that a
 // scan needs one barrier (two scans later every wave has read the first).
+template <int NT>
 struct WaveSums {
-    uint32_t (*part)[kEvWaves];                            // [2] in LDS
+    static constexpr int kWaves = NT / 64;
+    uint32_t (*part)[kWaves];                            // [2] in LDS
     int at = 0;
     // (sum over the waves before this one, over all of them) of a value that
     // lane 63 of each wave gives
@@ -73,7 +77,7 @@ struct WaveSums {
         uint32_t before = 0;
         total = 0;
 #pragma unroll
-        for (int i = 0; i < kEvWaves; i++) {
+        for (int i = 0; i < kWaves; i++) {
             const uint32_t x = p[i];
             before += i < wave ? x : 0;
             total += x;
@@ -135,9 +139,10 @@ struct Digits {
 };
 
 // Histogram of digit `level` of the rows that agree with the digits so far.
+template <int NT>
 __device__ __forceinline__ void count_digit(const Rows &r, const Digits &d, int level,
                                             uint32_t *s_hist) {
-    for (int i = threadIdx.x; i < kEvBins; i += kEvThreads)
+    for (int i = threadIdx.x; i < kEvBins; i += NT)
         s_hist[i] = 0;
     __syncthreads();
 #pragma unroll
@@ -149,16 +154,24 @@ __device__ __forceinline__ void count_digit(const Rows &r, const Digits &d, int 
     __syncthreads();
 }
 
-// The bin in which the `left`-th largest lies, from this thread's bins 2047 -
-// 2 tid (c0) and 2046 - 2 tid (c1); s_pick: the bin and how many of it stay.
-__device__ __forceinline__ void pick_bin(uint32_t c0, uint32_t c1, uint32_t left, WaveSums &sums,
+// The bin in which the `left`-th largest lies, from this thread's bins (c[i]:
+// bin 2047 - N tid - i); s_pick: the bin and how many of it stay.
+template <int NT, int N>
+__device__ __forceinline__ void pick_bin(const uint32_t (&c)[N], uint32_t left, WaveSums<NT> &sums,
                                          uint32_t *s_pick) {
-    uint32_t total;
-    const uint32_t above = sums.scan(c0 + c1, total);
-    if (above < left && left <= above + c0 + c1) {
-        const bool first = left <= above + c0;
-        s_pick[0] = kEvBins - 1 - 2 * threadIdx.x - (first ? 0 : 1);
-        s_pick[1] = left - above - (first ? 0 : c0);
+    static_assert(N * NT == kEvBins, "every bin has a thread");
+    uint32_t mine = 0, total;
+#pragma unroll
+    for (int i = 0; i < N; i++)
+        mine += c[i];
+    uint32_t above = sums.scan(mine, total);
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+        if (above < left && left <= above + c[i]) {
+            s_pick[0] = kEvBins - 1 - N * threadIdx.x - i;
+            s_pick[1] = left - above;
+        }
+        above += c[i];
     }
     __syncthreads();
 }
@@ -166,9 +179,10 @@ __device__ __forceinline__ void pick_bin(uint32_t c0, uint32_t c1, uint32_t left
 // Places of a part's rows: all of them, or those above the pivot and the
 // first `need` equal to it; gt0, eq0: such rows before the part.  The masks of
 // 64 rows stay in scalar registers between the count and the placing.
+template <int NT>
 __device__ __forceinline__ void place(const EvictArgs &a, const Choice &c, const Rows &r, bool all,
                                       uint32_t pivot, uint32_t need, uint32_t gt0, uint32_t eq0,
-                                      uint32_t off, WaveSums &sums) {
+                                      uint32_t off, WaveSums<NT> &sums) {
     uint64_t gm[kEvPer], em[kEvPer];
     uint32_t gt = 0, eq = 0;                               // of this wave
     const int left = c.old - uni(r.first);                 // (lane 0's row)
@@ -209,6 +223,7 @@ __device__ __forceinline__ void place(const EvictArgs &a, const Choice &c, const
 
 // Rows that the sequences before this one keep; cu_keep; the newest rows, of
 // which workgroup `part` of `parts` places its share.
+template <int NT>
 __device__ __forceinline__ uint32_t place_recent(const EvictArgs &a, const Choice &c, int part,
                                                  int parts) {
     const int tid = threadIdx.x;
@@ -223,33 +238,40 @@ __device__ __forceinline__ uint32_t place_recent(const EvictArgs &a, const Choic
     }
     const int64_t out = (int64_t)c.h * a.cap + off + c.k;
     const int room = a.cap - (int)off - c.k;
-    for (int64_t i = part * kEvThreads + tid; i < min(c.rec, room); i += parts * kEvThreads) {
+    // (unsigned: a step past the end may pass 2^31)
+    const uint32_t end = max(0, min(c.rec, room));
+    for (uint32_t i = part * NT + tid; i < end; i += parts * NT) {
         a.keep_idx[out + i] = c.base + c.old + (int)i;
         a.score_out[out + i] = c.score[c.old + i];
     }
     return off;
 }
 
-__global__ __launch_bounds__(kEvThreads) void evict_select_kernel(const EvictArgs a) {
-    __shared__ uint32_t s_hist[kEvBins], s_part[2][kEvWaves], s_pick[2];
+template <int NT>
+__global__ __launch_bounds__(NT) void evict_select_kernel(const EvictArgs a) {
+    constexpr int N = kEvBins / NT;
+    __shared__ uint32_t s_hist[kEvBins], s_part[2][NT / 64], s_pick[2];
     const int tid = threadIdx.x;
-    WaveSums sums{s_part};
+    WaveSums<NT> sums{s_part};
     const Choice c(a, blockIdx.x);
     const Rows r(c, 0);
-    const uint32_t off = place_recent(a, c, 0, 1);
+    const uint32_t off = place_recent<NT>(a, c, 0, 1);
     Digits d;
     d.left = c.k;
     if (c.by_score()) {
 #pragma unroll 1
         for (int level = 0; level < 3; level++) {
-            count_digit(r, d, level, s_hist);
-            pick_bin(s_hist[kEvBins - 1 - 2 * tid], s_hist[kEvBins - 2 - 2 * tid], d.left, sums,
-                     s_pick);
+            count_digit<NT>(r, d, level, s_hist);
+            uint32_t bins[N];
+#pragma unroll
+            for (int i = 0; i < N; i++)
+                bins[i] = s_hist[kEvBins - 1 - N * tid - i];
+            pick_bin<NT, N>(bins, d.left, sums, s_pick);
             d.take(level, s_pick[0], s_pick[1]);
         }
     }
     if (c.k > 0)
-        place(a, c, r, c.k == c.old, d.prefix, d.left, 0, 0, off, sums);
+        place<NT>(a, c, r, c.k == c.old, d.prefix, d.left, 0, 0, off, sums);
 }
 
 // Two 16-bit bins per word: word 1023 - t holds thread t's bins.
@@ -260,7 +282,7 @@ __device__ __forceinline__ uint32_t *hist_of(const EvictArgs &a, int level, int 
 // This thread's bins over all parts with rows by score, and over those before
 // `part`.
 struct Bins {
-    uint32_t c0 = 0, c1 = 0, before0 = 0, before1 = 0;
+    uint32_t sum[2] = {0, 0}, before0 = 0, before1 = 0;
     __device__ __forceinline__ Bins(const EvictArgs &a, const Choice &c, int level, int problem,
                                     int part) {
         const int n = (c.old + kEvPartRows - 1) / kEvPartRows;
@@ -268,8 +290,8 @@ struct Bins {
 #pragma unroll 8
         for (int i = 0; i < n; i++) {
             const uint32_t v = w[(int64_t)i * (kEvBins / 2)];
-            c0 += v >> 16;
-            c1 += v & 0xFFFFu;
+            sum[0] += v >> 16;
+            sum[1] += v & 0xFFFFu;
             before0 += i < part ? v >> 16 : 0u;
             before1 += i < part ? v & 0xFFFFu : 0u;
         }
@@ -281,9 +303,9 @@ struct Bins {
 // rows above the last pick are counted, and its digit LEVEL.
 template <int LEVEL>
 __global__ __launch_bounds__(kEvThreads) void evict_hist_kernel(const EvictArgs a) {
-    __shared__ uint32_t s_hist[kEvBins], s_part[2][kEvWaves], s_pick[2];
+    __shared__ uint32_t s_hist[kEvBins], s_part[2][kEvThreads / 64], s_pick[2];
     const int tid = threadIdx.x;
-    WaveSums sums{s_part};
+    WaveSums<kEvThreads> sums{s_part};
     const int problem = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
     const Choice c(a, problem);
     if (!c.by_score() || (int64_t)part * kEvPartRows >= c.old)
@@ -295,7 +317,7 @@ __global__ __launch_bounds__(kEvThreads) void evict_hist_kernel(const EvictArgs 
         d.take(0, a.picks[problem * 2], a.picks[problem * 2 + 1]);
     if constexpr (LEVEL > 0) {
         const Bins w(a, c, LEVEL - 1, problem, part);
-        pick_bin(w.c0, w.c1, d.left, sums, s_pick);
+        pick_bin<kEvThreads, 2>(w.sum, d.left, sums, s_pick);
         if (LEVEL == 1 && part == 0 && tid < 2)
             a.picks[problem * 2 + tid] = s_pick[tid];
         const Digits last = d;
@@ -314,7 +336,7 @@ __global__ __launch_bounds__(kEvThreads) void evict_hist_kernel(const EvictArgs 
             *above = (LEVEL == 1 ? 0u : *above) + total;
         }
     }
-    count_digit(r, d, LEVEL, s_hist);
+    count_digit<kEvThreads>(r, d, LEVEL, s_hist);
     hist_of(a, LEVEL, problem, part)[kEvBins / 2 - 1 - tid] =
         s_hist[kEvBins - 1 - 2 * tid] << 16 | s_hist[kEvBins - 2 - 2 * tid];
     if (LEVEL == 2 && part == 0 && tid < 2)
@@ -322,12 +344,12 @@ __global__ __launch_bounds__(kEvThreads) void evict_hist_kernel(const EvictArgs 
 }
 
 __global__ __launch_bounds__(kEvThreads) void evict_rank_kernel(const EvictArgs a) {
-    __shared__ uint32_t s_part[2][kEvWaves], s_pick[2];
+    __shared__ uint32_t s_part[2][kEvThreads / 64], s_pick[2];
     const int tid = threadIdx.x;
-    WaveSums sums{s_part};
+    WaveSums<kEvThreads> sums{s_part};
     const int problem = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
     const Choice c(a, problem);
-    const uint32_t off = place_recent(a, c, part, a.parts);
+    const uint32_t off = place_recent<kEvThreads>(a, c, part, a.parts);
     if (c.k == 0 || (int64_t)part * kEvPartRows >= c.old)
         return;
     const Rows r(c, part);
@@ -339,7 +361,7 @@ __global__ __launch_bounds__(kEvThreads) void evict_rank_kernel(const EvictArgs 
         picks += a.num_seqs * a.hkv * 2;
         d.take(1, picks[0], picks[1]);
         const Bins w(a, c, 2, problem, part);
-        pick_bin(w.c0, w.c1, d.left, sums, s_pick);
+        pick_bin<kEvThreads, 2>(w.sum, d.left, sums, s_pick);
         // rows of the parts before this one: above the pick of each digit,
         // and equal to the pivot
         const uint32_t b0 = kEvBins - 1 - 2 * tid, bin = s_pick[0];
@@ -352,7 +374,7 @@ __global__ __launch_bounds__(kEvThreads) void evict_rank_kernel(const EvictArgs 
     } else {
         gt0 = (uint32_t)part * kEvPartRows;
     }
-    place(a, c, r, c.k == c.old, d.prefix, d.left, gt0, eq0, off, sums);
+    place<kEvThreads>(a, c, r, c.k == c.old, d.prefix, d.left, gt0, eq0, off, sums);
 }
 
 template <int D>
@@ -377,8 +399,12 @@ __global__ __launch_bounds__(256) void evict_copy_kernel(const EvictArgs a) {
 hipError_t launch_cache_evict(const EvictArgs &a, hipStream_t s) {
     const dim3 grid_s(a.num_seqs * a.hkv * a.parts), block(kEvThreads);
     hipError_t e;
-    if (a.parts == 1) {
-        hipLaunchKernelGGL(evict_select_kernel, grid_s, block, 0, s, a);
+    if (a.small) {
+        hipLaunchKernelGGL((evict_select_kernel<kEvSmallRows / kEvPer>), grid_s,
+                           dim3(kEvSmallRows / kEvPer), 0, s, a);
+        e = hipGetLastError();
+    } else if (a.parts == 1) {
+        hipLaunchKernelGGL((evict_select_kernel<kEvThreads>), grid_s, block, 0, s, a);
         e = hipGetLastError();
     } else {
         hipLaunchKernelGGL((evict_hist_kernel<0>), grid_s, block, 0, s, a);

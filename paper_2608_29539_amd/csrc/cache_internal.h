@@ -87,9 +87,11 @@ struct EvictArgs {
     // histograms [2][B Hkv][parts][1024], two picks [2][B Hkv][2], rows above
     // them [B Hkv][parts]
     int32_t parts;
+    int32_t small;                           // no cache of more than kEvSmallRows
     uint32_t *hist, *picks, *above;
 };
 constexpr int kEvPartRows = 8192;
+constexpr int kEvSmallRows = 2048;
 hipError_t launch_cache_evict(const EvictArgs &a, hipStream_t s);
 
 }  // namespace logo

@@ -2044,6 +2044,7 @@ logo_status logo_cache_evict(const logo_problem *p, const float *score, int32_t 
     a.keep_idx = keep_idx;
     a.cu_keep = cu_keep;
     a.parts = (int32_t)d.parts;
+    a.small = p->max_seqlen <= kEvSmallRows;
     a.hist = (uint32_t *)ws;
     a.picks = (uint32_t *)((char *)ws + d.picks);
     a.above = (uint32_t *)((char *)ws + d.above);
