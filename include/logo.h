@@ -488,12 +488,12 @@ typedef struct {
  *              the four caches together, or both (NULL = the local ones);
  *              LOGO_ERR_ARG for some of the caches without the others.
  *   All bf16 tensors 16-byte aligned (LOGO_ERR_ARG).
- *   The values of a prefix must be finite: one that is not may reach, through
+ *   The values must be finite: one of a prefix that is not may reach, through
  *   a product with a zero weight, sequences of its group whose window leaves
- *   it out.
- *   Numerics: P is rounded to bf16 for the product with V (as in
- *   logo_attn_fwd), everything else is fp32; the result does not depend on
- *   the order in which workgroups run.
+ *   it out, and an infinite one makes every channel of its head NaN.
+ *   Numerics: P goes into the product with V as the sum of two bf16 numbers
+ *   (2^-16 of its value is lost), everything else is fp32; the result does not
+ *   depend on the order in which workgroups run.
  *   ws >= logo_decode_prefix_workspace_bytes(p, prefix) bytes, 256-byte
  *   aligned (partial results of the key chunks).
  */

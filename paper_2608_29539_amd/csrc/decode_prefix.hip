@@ -23,8 +23,12 @@
 //   prefix_combine_kernel  joins the chunks of each (sequence, head), applies
 //                          ContextNorm and the fusion, rounds once to bf16.
 //
-// P is rounded to bf16 for the PV product, as in the layer's kernels (its row
-// sum takes the rounded values); everything else is fp32.
+// The decoding step keeps P in fp32, and so does this one but for 2^-16 of it: P
+// goes into the PV product as the sum of two bf16 numbers, two products per
+// fragment of V.  One would halve those products (64 sequences behind 32K tokens,
+// all selected: 76 us a step, 89 with two; 32 behind 16K, 4 selected: 47 both
+// ways) but leave an error as large as the output's rounding.  Everything else
+// is fp32.
 //
 // Bounds (32 / 8 heads, d = 128).  32 sequences behind 16K tokens, 4 selected:
 // reading 171 MB, 31 us + 5.9 of merge (5.5 TB/s from the last-level cache).
@@ -96,6 +100,12 @@ __device__ __forceinline__ int wave_max(int x) {
 
 // Kinds of key range (the order of the work items).
 enum { kPfxGlobal = 0, kOwnGlobal = 1, kPfxLocal = 2, kOwnLocal = 3 };
+
+// Two weights as bf16 parts, x = hi + lo to 2^-16 of its value.
+__device__ __forceinline__ void split_bf16x2(float x, float y, bf16x2 &hi, bf16x2 &lo) {
+    hi = cvt_bf16x2(x, y);
+    lo = cvt_bf16x2(x - (float)hi[0], y - (float)hi[1]);
+}
 
 // Keys [lo, hi) of range `kind` that a sequence with P prefix rows and S rows
 // of its own sees, in rows of the prefix or of the sequence.
@@ -291,7 +301,6 @@ __global__ __launch_bounds__(kPrefixThreads, 2) void prefix_attn_kernel(const Pr
     // keys that every row of the wave sees: tiles inside need no mask
     const int all_lo = uni(wave_max(lo)), all_hi = -uni(wave_max(-hi));
     const float sc = a.scale_log2;
-    const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
     const int64_t prow = ((int64_t)(a.slot0[kind] + c) * a.num_seqs + b) * a.hq + head;
     float m_ref = kNegInf, l_run = 0.f;
     // the running max of a tile's scores moves (rescaling O and l) when it is
@@ -382,21 +391,29 @@ __global__ __launch_bounds__(kPrefixThreads, 2) void prefix_attn_kernel(const Pr
                             max2(max2(s[1][0], s[1][1]), max2(s[1][2], s[1][3])));
             mx = quad_max(mx) * sc;
             const float mc = rescale(mx, acc);
-            bf16x8 pf;
+            bf16x8 pf[2];                            // the weights' upper and lower parts
+            float l2[2] = {};
 #pragma unroll
             for (int h = 0; h < 2; h++)
 #pragma unroll
                 for (int i = 0; i < 4; i += 2) {
-                    const bf16x2 p =
-                        cvt_bf16x2(__builtin_amdgcn_exp2f(fmaf(s[h][i], sc, -mc)),
-                                   __builtin_amdgcn_exp2f(fmaf(s[h][i + 1], sc, -mc)));
-                    l_run = __builtin_amdgcn_fdot2_f32_bf16(p, ones, l_run, false);
-                    pf[h * 4 + i] = p[0];
-                    pf[h * 4 + i + 1] = p[1];
-                }
+                    const float x = __builtin_amdgcn_exp2f(fmaf(s[h][i], sc, -mc));
+                    const float y = __builtin_amdgcn_exp2f(fmaf(s[h][i + 1], sc, -mc));
+                    bf16x2 p[2];
+                    split_bf16x2(x, y, p[0], p[1]);
+                    l2[i >> 1] += x + y;
 #pragma unroll
-            for (int x = 0; x < D / 16; x++)
-                acc[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[x], pf, acc[x], 0, 0, 0);
+                    for (int u = 0; u < 2; u++) {
+                        pf[u][h * 4 + i] = p[u][0];
+                        pf[u][h * 4 + i + 1] = p[u][1];
+                    }
+                }
+            l_run += l2[0] + l2[1];
+#pragma unroll
+            for (int u = 0; u < 2; u++)
+#pragma unroll
+                for (int x = 0; x < D / 16; x++)
+                    acc[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[x], pf[u], acc[x], 0, 0, 0);
         }
         // The waves' (O, m, l) joined through LDS (the stages are read): wave w
         // takes its quarter of the blocks.
@@ -503,15 +520,15 @@ __global__ __launch_bounds__(kPrefixThreads, 2) void prefix_attn_kernel(const Pr
         v_frags(buf, 0, vf[0]);
         __builtin_amdgcn_sched_barrier(0);
         f32x16 next = scores(f32x16{}, 0, kf[0]);
-        bf16x2 pw[8];
-        float l2 = 0.f;
+        bf16x2 pw[2][8];                         // the weights' upper and lower parts
+        float l2[2] = {};
         auto exps = [&](int i0) {
 #pragma unroll
             for (int i = i0; i < i0 + 8; i += 2) {
-                pw[i >> 1] = cvt_bf16x2(__builtin_amdgcn_exp2f(fmaf(s[i], sc, -mc)),
-                                        __builtin_amdgcn_exp2f(fmaf(s[i + 1], sc, -mc)));
-                float &lx = (i & 2) ? l2 : l_run;
-                lx = __builtin_amdgcn_fdot2_f32_bf16(pw[i >> 1], ones, lx, false);
+                const float x = __builtin_amdgcn_exp2f(fmaf(s[i], sc, -mc));
+                const float y = __builtin_amdgcn_exp2f(fmaf(s[i + 1], sc, -mc));
+                split_bf16x2(x, y, pw[0][i >> 1], pw[1][i >> 1]);
+                l2[(i >> 1) & 1] += x + y;
             }
         };
         exps(0);
@@ -519,19 +536,22 @@ __global__ __launch_bounds__(kPrefixThreads, 2) void prefix_attn_kernel(const Pr
         __builtin_amdgcn_sched_barrier(0);
         next = scores(next, kHalf, kf[1]);
         exps(8);
-        l_run += l2;
+        l_run += l2[0] + l2[1];
 #pragma unroll
-        for (int ss = 0; ss < 2; ss++) {
-            bf16x8 pf;
+        for (int ss = 0; ss < 2; ss++)
 #pragma unroll
-            for (int j = 0; j < 4; j++) {
-                pf[2 * j] = pw[ss * 4 + j][0];
-                pf[2 * j + 1] = pw[ss * 4 + j][1];
+            for (int u = 0; u < 2; u++) {
+                bf16x8 pf;
+#pragma unroll
+                for (int j = 0; j < 4; j++) {
+                    pf[2 * j] = pw[u][ss * 4 + j][0];
+                    pf[2 * j + 1] = pw[u][ss * 4 + j][1];
+                }
+#pragma unroll
+                for (int cb = 0; cb < D / 32; cb++)
+                    acc[cb] =
+                        __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[ss][cb], pf, acc[cb], 0, 0, 0);
             }
-#pragma unroll
-            for (int cb = 0; cb < D / 32; cb++)
-                acc[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[ss][cb], pf, acc[cb], 0, 0, 0);
-        }
         s = next;
     };
 
