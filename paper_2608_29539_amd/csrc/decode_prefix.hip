@@ -760,11 +760,14 @@ __global__ __launch_bounds__(256) void prefix_combine_kernel(const PrefixArgs a)
 
 template <int D>
 hipError_t launch_d(const PrefixArgs &a, hipStream_t s) {
-    hipLaunchKernelGGL((prefix_attn_kernel<D>), dim3(a.first[4] + (a.act || a.n_act)),
-                       dim3(kPrefixThreads), 0, s, a);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess)
-        return e;
+    // (no work item where no cache has any row: the merge writes the zeros)
+    const int items = a.first[4] + (a.act || a.n_act);
+    if (items > 0) {
+        hipLaunchKernelGGL((prefix_attn_kernel<D>), dim3(items), dim3(kPrefixThreads), 0, s, a);
+        hipError_t e = hipGetLastError();
+        if (e != hipSuccess)
+            return e;
+    }
     const int64_t jobs = (int64_t)a.num_seqs * a.hq;
     // four waves per head where a head has many chunks and the heads alone do
     // not fill the card (64 sequences of 32 heads behind 32K tokens, 2048 heads:

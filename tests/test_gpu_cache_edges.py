@@ -1,0 +1,48 @@
+"""GPU tests of the cache operators at the ends of what their documentation
+allows."""
+import math
+
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def pk():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.fail("no GPU visible: the gpu tests need an MI355X")
+    import paper_2608_29539_amd as pk
+    pk.library()
+    return pk
+
+
+def bf16(rng, *shape):
+    import torch
+    return torch.from_numpy(rng.standard_normal(shape).astype(np.float32)).cuda().to(torch.bfloat16)
+
+
+@pytest.mark.parametrize("lists", [False, True], ids=["output-alone", "lists"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_prefix_no_cache_has_a_row(pk, d, lists):
+    """Without host copies, a batch of empty caches behind empty prefixes
+    outputs zeros, and lists its selected sequences."""
+    import torch
+    cu = torch.zeros(4, dtype=torch.int32, device="cuda")
+    grp = torch.tensor([0, 2, 3], dtype=torch.int32, device="cuda")
+    prob = pk.Problem(cu, 4, 2, d, 8, total_tokens=0, max_seqlen=0)
+    pre = pk.Prefix(cu[:3].clone(), grp, total_tokens=0, max_prefix=0, max_group=2)
+    q, none = bf16(np.random.default_rng(1), 3, 4, d), torch.empty((0, 2, d), dtype=torch.bfloat16,
+                                                                  device="cuda")
+    gate = torch.tensor([0.7, 0.2, 0.9], device="cuda")
+    out = torch.full((3, 4, d), 5.0, dtype=torch.bfloat16, device="cuda")
+    kw = {}
+    if lists:
+        kw = dict(active=torch.full((3,), -7, dtype=torch.int32, device="cuda"),
+                  n_active=torch.full((1,), -7, dtype=torch.int32, device="cuda"))
+    pk.logo_decode_prefix(prob, pre, q, none, none, none, none, gate, threshold=0.5, out=out, **kw)
+    torch.cuda.synchronize()
+    assert bool((out == 0).all())
+    if lists:
+        assert kw["active"].tolist() == [0, 2, -7] and kw["n_active"].tolist() == [2]
