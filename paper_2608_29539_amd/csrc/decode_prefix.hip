@@ -742,7 +742,8 @@ __global__ __launch_bounds__(256) void prefix_combine_kernel(const PrefixArgs a)
         ss = row_sum(ss);
         if (D == 128)                            // (32 lanes: two rows)
             ss += __shfl_xor(ss, 16, 64);
-        const float rn = 1.f / sqrtf(ss / (float)D + a.eps);
+        // (a sequence without rows: zeros, also where eps is zero)
+        const float rn = lsum == 0.f ? 0.f : 1.f / sqrtf(ss / (float)D + a.eps);
 #pragma unroll
         for (int i = 0; i < 4; i++)
             o[i] *= rn * (gain ? gain[h * D + 4 * e + i] : 1.f);

@@ -46,3 +46,25 @@ def test_prefix_no_cache_has_a_row(pk, d, lists):
     assert bool((out == 0).all())
     if lists:
         assert kw["active"].tolist() == [0, 2, -7] and kw["n_active"].tolist() == [2]
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("thr", [-math.inf, math.inf], ids=["global", "local"])
+def test_prefix_empty_cache_without_eps(pk, d, thr):
+    """Zeros for a sequence without rows also where eps = 0 would divide them
+    by zero; its neighbour's output stays."""
+    import torch
+    rng = np.random.default_rng(2)
+    cu, cup = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in ([0, 0, 5], [0, 0, 30]))
+    grp = torch.tensor([0, 1, 2], dtype=torch.int32, device="cuda")
+    prob = pk.Problem(cu, 4, 2, d, 8, total_tokens=5, max_seqlen=5)
+    pre = pk.Prefix(cup, grp, total_tokens=30, max_prefix=30, max_group=1)
+    q, gate = bf16(rng, 2, 4, d), torch.tensor([0.7, 0.4], device="cuda")
+    t = [bf16(rng, n, 2, d) for n in (30, 30, 5, 5)]
+    got = {eps: pk.logo_decode_prefix(prob, pre, q, *t, gate, threshold=thr, eps=eps)[0]
+           for eps in (0.0, 1e-12)}
+    torch.cuda.synchronize()
+    assert bool((got[0.0][0] == 0).all())
+    assert bool(torch.isfinite(got[0.0]).all()) and bool((got[0.0][1] != 0).any())
+    # (1e-12 in a mean square near one moves no bf16 rounding but a tie's)
+    assert bool(((got[0.0] - got[1e-12]).float().abs() <= 2.0 ** -7 * got[0.0].float().abs()).all())
