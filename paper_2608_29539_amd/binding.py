@@ -171,6 +171,14 @@ def logo_version() -> str:
     return library().logo_version().decode()
 
 
+def _cu_fault(t, name):
+    """What keeps t from being read as packed int32 bounds, or None."""
+    import torch
+    if t.dtype != torch.int32:
+        return f"{name}: expected {torch.int32}, got {t.dtype}"
+    return None if t.is_contiguous() else f"{name} must be contiguous"
+
+
 class Problem:
     """Host description of a packed varlen problem (mirrors ``logo_problem``).
 
@@ -185,6 +193,7 @@ class Problem:
                  softmax_scale: float = 0.0):
         import numpy as np
         self.cu_seqlens = cu_seqlens
+        self._cu_fault = _cu_fault(cu_seqlens, "cu_seqlens")   # (the cache operators refuse it)
         host = None
         if cu_seqlens_host is not None:
             host = np.ascontiguousarray(np.asarray(
@@ -231,6 +240,9 @@ class Prefix:
             return np.ascontiguousarray(np.asarray(x.cpu() if hasattr(x, "cpu") else x),
                                         dtype=np.int32)
 
+        for t, nm in ((cu_prefix, "cu_prefix"), (cu_group, "cu_group")):
+            if _cu_fault(t, nm):
+                raise TypeError(_cu_fault(t, nm))
         self.cu_prefix, self.cu_group = cu_prefix, cu_group
         R = int(cu_prefix.numel()) - 1
         if int(cu_group.numel()) - 1 != R:
@@ -803,11 +815,13 @@ def logo_decode_noalloc(prob: Problem, q, k, v, gate, out, *, threshold: Optiona
     return out, active, n_active
 
 
-def _checks_here():
+def _checks_here(prob: Problem):
     """``_check`` that also refuses tensors of another device than the current
     one, whose stream the call would run on, and the same for tensors of which
     nothing else is checked."""
     import torch
+    if prob._cu_fault:
+        raise TypeError(prob._cu_fault)
     dev = torch.cuda.current_device() if torch.cuda.is_initialized() else None
 
     def here(*tensors):
@@ -858,7 +872,7 @@ def logo_decode_prefix(prob: Problem, prefix: Prefix, q, k_pre, v_pre, k, v, gat
                         prob.num_seqs)
     P = prefix.total_tokens
     mode = _step_threshold(threshold, threshold_device)
-    check, here = _checks_here()
+    check, here = _checks_here(prob)
     check(q, torch.bfloat16, (B, Hq, d), "q")
     for t, nm, n in ((k_pre, "k_pre", P), (v_pre, "v_pre", P), (k, "k", N), (v, "v", N)):
         check(t, torch.bfloat16, (n, Hkv, d), nm)
@@ -909,7 +923,7 @@ def logo_cache_score(prob: Problem, q, k, *, sel_idx=None, cu_sel=None, lse=None
     the forward's base-2 log-sum-exp; without it it is computed."""
     import torch
     N, Hq, Hkv, d = prob.total_tokens, prob.num_q_heads, prob.num_kv_heads, prob.head_dim
-    check, here = _checks_here()
+    check, here = _checks_here(prob)
     check(q, torch.bfloat16, (N, Hq, d), "q")
     check(k, torch.bfloat16, (N, Hkv, d), "k")
     if (sel_idx is None) != (cu_sel is None):
@@ -940,7 +954,7 @@ def logo_decode_score(prob: Problem, q, k, gate, *, threshold: Optional[float] =
     N, Hq, Hkv, d, B = (prob.total_tokens, prob.num_q_heads, prob.num_kv_heads, prob.head_dim,
                         prob.num_seqs)
     mode = _step_threshold(threshold, threshold_device)
-    check, here = _checks_here()
+    check, here = _checks_here(prob)
     check(q, torch.bfloat16, (B, Hq, d), "q")
     check(k, torch.bfloat16, (N, Hkv, d), "k")
     check(gate, torch.float32, (B,), "gate")
@@ -967,7 +981,7 @@ def logo_cache_evict(prob: Problem, score, budget: int, *, recent: int = 0, k=No
     v_g_out (None without their inputs), score_out, keep_idx and cu_keep."""
     import torch
     N, Hkv, d, B = prob.total_tokens, prob.num_kv_heads, prob.head_dim, prob.num_seqs
-    check, here = _checks_here()
+    check, here = _checks_here(prob)
     check(score, torch.float32, (Hkv, N), "score")
     cap = None
     for t, dim in ((score_out, 1), (keep_idx, 1), (k_out, 0), (v_out, 0), (k_g_out, 0),
