@@ -824,10 +824,14 @@ def _checks_here(prob: Problem):
         raise TypeError(prob._cu_fault)
     dev = torch.cuda.current_device() if torch.cuda.is_initialized() else None
 
-    def here(*tensors):
+    def here(*tensors, ws=None):
         for t in tensors:
             if t is not None and t.get_device() != dev:
                 raise ValueError(f"tensor on {t.device}, but the current device is {dev}")
+        if ws is not None:
+            here(ws)
+            if not ws.is_contiguous():           # (its numel() bytes lie behind each other)
+                raise ValueError("ws must be contiguous")
 
     def check(t, dtype, shape, name):
         if (t is not None and t.dtype == dtype and t.get_device() == dev and t.is_contiguous()
@@ -895,7 +899,7 @@ def logo_decode_prefix(prob: Problem, prefix: Prefix, q, k_pre, v_pre, k, v, gat
     if ws is None:
         ws = torch.empty(logo_decode_prefix_workspace_bytes(prob, prefix), dtype=torch.uint8,
                          device=q.device)
-    here(threshold_device, ws, prob.cu_seqlens, prefix.cu_prefix, prefix.cu_group)
+    here(threshold_device, prob.cu_seqlens, prefix.cu_prefix, prefix.cu_group, ws=ws)
     _call("logo_decode_prefix", prob.c, prefix.c, _ptr(q), _ptr(k_pre), _ptr(v_pre), _ptr(k),
           _ptr(v), _ptr(q_g), _ptr(k_pre_g), _ptr(v_pre_g), _ptr(k_g), _ptr(v_g), _ptr(gate),
           mode, float(threshold if threshold is not None else 0.0), _ptr(threshold_device),
@@ -939,7 +943,7 @@ def logo_cache_score(prob: Problem, q, k, *, sel_idx=None, cu_sel=None, lse=None
     nbytes = 0
     if lse is None:
         ws, nbytes = _ws(prob, LOGO_ENTRY_CACHE_SCORE, cap, ws)
-    here(ws, prob.cu_seqlens)
+    here(prob.cu_seqlens, ws=ws)
     _call("logo_cache_score", prob.c, _ptr(q), _ptr(k), _ptr(sel_idx), _ptr(cu_sel), int(cap),
           _ptr(lse), _ptr(score_in), _ptr(score), _ptr(ws), nbytes, _stream())
     return score
@@ -960,7 +964,7 @@ def logo_decode_score(prob: Problem, q, k, gate, *, threshold: Optional[float] =
     check(gate, torch.float32, (B,), "gate")
     score = _check_scores(check, prob, score_in, score, q.device)
     ws, nbytes = _ws(prob, LOGO_ENTRY_DECODE_SCORE, 0, ws)
-    here(threshold_device, ws, prob.cu_seqlens)
+    here(threshold_device, prob.cu_seqlens, ws=ws)
     _call("logo_decode_score", prob.c, _ptr(q), _ptr(k), _ptr(gate), mode,
           float(threshold if threshold is not None else 0.0), _ptr(threshold_device),
           _ptr(score_in), _ptr(score), _ptr(ws), nbytes, _stream())
@@ -991,7 +995,7 @@ def logo_cache_evict(prob: Problem, score, budget: int, *, recent: int = 0, k=No
             break
     if cap is None:
         cap = max(logo_cache_keep_capacity(prob, budget), 0)
-    here(ws, prob.cu_seqlens)
+    here(prob.cu_seqlens, ws=ws)
 
     def rows(t, o, nm):
         if t is not None:

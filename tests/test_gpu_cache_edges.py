@@ -68,3 +68,24 @@ def test_prefix_empty_cache_without_eps(pk, d, thr):
     assert bool(torch.isfinite(got[0.0]).all()) and bool((got[0.0][1] != 0).any())
     # (1e-12 in a mean square near one moves no bf16 rounding but a tie's)
     assert bool(((got[0.0] - got[1e-12]).float().abs() <= 2.0 ** -7 * got[0.0].float().abs()).all())
+
+
+def test_workspace_of_one_stored_byte(pk):
+    """An expanded workspace has the bytes that are asked for, but not the
+    memory: every operator refuses it."""
+    import torch
+    rng = np.random.default_rng(3)
+    n = 20000                                    # (more rows than an eviction's part)
+    cu = torch.tensor([0, n], dtype=torch.int32, device="cuda")
+    one = torch.tensor([0, 1], dtype=torch.int32, device="cuda")
+    prob = pk.Problem(cu, 2, 2, 64, 8, cu_seqlens_host=[0, n])
+    pre = pk.Prefix(cu, one, cu_prefix_host=[0, n], cu_group_host=[0, 1])
+    q, qn, k = bf16(rng, 1, 2, 64), bf16(rng, n, 2, 64), bf16(rng, n, 2, 64)
+    gate, score = torch.ones(1, device="cuda"), torch.rand((2, n), device="cuda")
+    ws = torch.zeros(1, dtype=torch.uint8, device="cuda").expand(1 << 30)
+    for call in (lambda: pk.logo_decode_prefix(prob, pre, q, k, k, k, k, gate, threshold=0.5, ws=ws),
+                 lambda: pk.logo_cache_score(prob, qn, k, ws=ws),
+                 lambda: pk.logo_decode_score(prob, q, k, gate, threshold=0.5, ws=ws),
+                 lambda: pk.logo_cache_evict(prob, score, 2, k=k, v=k, ws=ws)):
+        with pytest.raises(ValueError, match="ws must be contiguous"):
+            call()
