@@ -495,7 +495,11 @@ typedef struct {
  *   (2^-16 of its value is lost), everything else is fp32; the result does not
  *   depend on the order in which workgroups run.
  *   ws >= logo_decode_prefix_workspace_bytes(p, prefix) bytes, 256-byte
- *   aligned (partial results of the key chunks).
+ *   aligned (partial results of the key chunks).  A smaller step's short chunks
+ *   may need more than a larger one's; a workspace of the size given for any
+ *   step of as many heads with no fewer sequences, longer caches and longer
+ *   prefixes is taken too: the keys then go in longer chunks, whose sums round
+ *   differently in fp32.
  */
 logo_status logo_decode_prefix(const logo_problem *p, const logo_prefix *prefix,
                                const logo_bf16 *q, const logo_bf16 *k_pre, const logo_bf16 *v_pre,
@@ -531,7 +535,12 @@ size_t logo_decode_prefix_workspace_bytes(const logo_problem *p, const logo_pref
  *   score      device [Hkv][N] fp32, every entry written.
  *   ws         only with lse NULL: >= logo_workspace_bytes(p,
  *              LOGO_ENTRY_CACHE_SCORE, sel_capacity) bytes, 256-byte aligned.
- * fp32 sums in a fixed order: the same call gives the same bits.
+ *              Few rows take more chunks of keys, and may need more of it than
+ *              many; a workspace of the size given for any larger sel_capacity
+ *              and longer sequences is taken too (longer chunks, whose sums
+ *              round differently in fp32).
+ * fp32 sums in a fixed order: the same call, with a workspace of the same size,
+ * gives the same bits.
  */
 logo_status logo_cache_score(const logo_problem *p, const logo_bf16 *q, const logo_bf16 *k,
                              const int32_t *sel_idx, const int32_t *cu_sel, int32_t sel_capacity,
@@ -547,7 +556,8 @@ logo_status logo_cache_score(const logo_problem *p, const logo_bf16 *q, const lo
  *              aligned (LOGO_ERR_ARG).
  *   score_in, score   as for logo_cache_score.
  *   ws >= logo_workspace_bytes(p, LOGO_ENTRY_DECODE_SCORE, 0) bytes, 256-byte
- *   aligned (the scores: 4 Hq N bytes and the chunks' sums).
+ *   aligned (the scores: 4 Hq N bytes and the chunks' sums).  The size given for
+ *   no fewer sequences with longer caches is taken too, as for logo_decode.
  */
 logo_status logo_decode_score(const logo_problem *p, const logo_bf16 *q, const logo_bf16 *k,
                               const float *gate, logo_sel_mode mode, float threshold,

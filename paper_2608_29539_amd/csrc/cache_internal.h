@@ -6,6 +6,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "cache_plan.h"
+
 namespace logo {
 
 // One decoding step of sequences that share prefixes (decode_prefix.hip).
@@ -14,8 +16,6 @@ namespace logo {
 // own part.  Partial results: (O [D], then m, l apart) per slot, sequence and
 // head, where chunk c of kind i has slot slot0[i] + c.
 constexpr int kPrefixThreads = 256;
-constexpr int kPrefixRows = 128;            // (sequence, head) rows per workgroup
-constexpr int kMaxPrefixChunks = 128;       // per kind
 constexpr int kWidePrefixMerge = 16;        // chunks above which a head's merge takes four waves
 struct PrefixArgs {
     const uint16_t *q, *k, *v, *kp, *vp;           // local branch: [B][Hq][d], own rows, prefixes
@@ -38,7 +38,6 @@ struct PrefixArgs {
 hipError_t launch_decode_prefix(const PrefixArgs &a, hipStream_t s);
 
 // Attention weight received by every key (cache_score.hip).
-constexpr int kLseRows = 128;               // flattened (rank, head) rows per workgroup
 struct ScoreArgs {
     const uint16_t *q, *k;
     const int32_t *cu, *sel_idx, *cu_sel;    // cu_sel NULL: every token is a row
@@ -55,7 +54,6 @@ struct ScoreArgs {
 };
 hipError_t launch_cache_score(const ScoreArgs &a, hipStream_t s);
 
-constexpr int kStepKeys = 1024;             // keys per workgroup of the weights' pass
 struct StepScoreArgs {
     const uint16_t *q, *k;
     const int32_t *cu;
@@ -90,7 +88,6 @@ struct EvictArgs {
     int32_t small;                           // no cache of more than kEvSmallRows
     uint32_t *hist, *picks, *above;
 };
-constexpr int kEvPartRows = 8192;
 constexpr int kEvSmallRows = 2048;
 hipError_t launch_cache_evict(const EvictArgs &a, hipStream_t s);
 

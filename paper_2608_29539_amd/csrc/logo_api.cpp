@@ -7,6 +7,7 @@
 #include "../../include/logo.h"
 #include "logo_internal.h"
 #include "cache_internal.h"
+#include "cache_plan.h"
 
 #include <algorithm>
 #include <cmath>
@@ -22,6 +23,8 @@ namespace {
 constexpr size_t kAlign = 256;
 
 size_t align_up(size_t x) { return (x + kAlign - 1) & ~(kAlign - 1); }
+static_assert(kPlanAlign == kAlign && kPlanXcds == kQueues && kPlanKeys == kBlockN,
+              "the plans of the cache operators are made for the kernels' tiles");
 
 bool debug_sync() {
     static const bool on = [] {
@@ -377,143 +380,6 @@ logo_status check_prefix(const logo_problem *p, const logo_prefix *x) {
         (long long)p->num_kv_heads * p->head_dim * 2 * kBlockN >= (1LL << 31))
         return LOGO_ERR_UNSUPPORTED;
     return LOGO_OK;
-}
-
-struct PrefixPlan {
-    int pfx_tiles, own_tiles;
-    int kc[4], chunks[4], slot0[4], slots;
-    long long first[5];
-    size_t ml, total;
-};
-
-// Keys per chunk.  The prefix's part of the global branch: about 320
-// workgroups over the KV heads and row tiles (one per CU and some, the other
-// ranges' beside them), at least 256 keys each: 32 sequences behind 16K tokens
-// 45.9 us (512 workgroups 49.9), 64 behind 32K 76.3 (256: 79.0, 512: 80.7, 128:
-// 122), three groups behind 17.6K in all 21.9 (384 of at least 128 keys: 25.6).
-// The sequences' own rows: 512 keys, 256 where that makes fewer than 512
-// workgroups (23 sequences, 2 KV heads: 32 and 24 us; 32 and 8: 38 and 39).
-// The window's part of a prefix: 256.  At most kMaxPrefixChunks each.
-PrefixPlan prefix_plan(const logo_problem *p, const logo_prefix *x, bool share) {
-    PrefixPlan d;
-    const long long G = p->num_q_heads / p->num_kv_heads, w = p->window;
-    const long long maxP = x->max_prefix, maxS = p->max_seqlen;
-    d.pfx_tiles = (int)(((long long)x->max_group * G + kPrefixRows - 1) / kPrefixRows);
-    d.own_tiles = (int)((G + kPrefixRows - 1) / kPrefixRows);
-    const long long span[4] = {maxP, share ? (maxS > w ? maxS - w : 0) : maxS,
-                               maxP < w ? maxP : w, maxS < w ? maxS : w};
-    const long long work = (long long)x->total_tokens * p->num_kv_heads * d.pfx_tiles;
-    const long long own_items = p->num_seqs * (long long)p->num_kv_heads * d.own_tiles *
-                                ((maxS + 511) / 512);
-    const long long own = own_items >= 512 ? 512 : 256;
-    const long long want[4] = {std::max(256LL, (work + 319) / 320), own, 256, own};
-    long long slots = 0, first = 0;
-    for (int i = 0; i < 4; i++) {
-        long long kc = std::max(want[i], (span[i] + kMaxPrefixChunks - 1) / kMaxPrefixChunks);
-        // (a position and a chunk behind it stay 32-bit)
-        kc = std::min((kc + kBlockN - 1) / kBlockN * kBlockN, 1LL << 26);
-        d.kc[i] = (int)kc;
-        d.chunks[i] = (int)((span[i] + kc - 1) / kc);
-        d.slot0[i] = (int)slots;
-        slots += d.chunks[i];
-        const bool is_own = i & 1;
-        const long long pairs = (long long)(is_own ? p->num_seqs : x->num_prefixes) * d.chunks[i] *
-                                p->num_kv_heads;
-        d.first[i] = first;
-        first += (pairs + kQueues - 1) / kQueues * kQueues * (is_own ? d.own_tiles : d.pfx_tiles);
-    }
-    d.first[4] = first;
-    d.slots = (int)slots;
-    const size_t rows = (size_t)slots * p->num_seqs * p->num_q_heads;
-    d.ml = align_up(sizeof(float) * rows * p->head_dim);
-    d.total = d.ml + align_up(sizeof(float) * 2 * rows);
-    return d;
-}
-
-struct ScorePlan {
-    int key_waves, lse_kc, lse_chunks, per_seq, lse_per_seq;
-    long long items, lse_items;
-    size_t total;
-};
-
-// Blocks of `block` over sequences of at most `longest` with `total` in all:
-// the same number for every sequence where that is at most twice the sum of
-// their own (a workgroup then finds its sequence by a division), else what
-// bounds the sum.
-long long score_blocks(long long total, long long longest, long long B, long long block,
-                       int &per_seq) {
-    const long long bound = total / block + B, each = (longest + block - 1) / block;
-    per_seq = each * B <= 2 * bound ? (int)each : 0;
-    return per_seq > 0 ? each * B : bound;
-}
-
-// Keys per workgroup (64, 128 or 256): the most that still makes 256
-// workgroups, one per CU.  More keys share the staged rows; fewer make up for
-// a small problem: 64 rows on 13324 keys, 8 KV heads, 21.8 us with 256 keys,
-// 29.5 with 128, 47.8 with 64; 256 rows on 1024 keys, 2 KV heads, d = 64, 29.3,
-// 20.4 and 14.7.  Key chunks of the log-sum-exp: about 1024 workgroups, of at least 512 keys.
-ScorePlan score_plan(const logo_problem *p, int32_t cap) {
-    ScorePlan d;
-    const long long N = p->total_tokens, B = p->num_seqs, H = p->num_kv_heads;
-    const long long G = p->num_q_heads / p->num_kv_heads;
-    d.key_waves = N * H >= 256 * 256 ? 4 : N * H >= 256 * 128 ? 2 : 1;
-    const long long maxL = std::max(1, p->max_seqlen);
-    d.items = score_blocks(N, maxL, B, 64 * d.key_waves, d.per_seq) * H;
-    // (one sequence may have all the rows, and a row may be listed twice)
-    const long long tiles = score_blocks(cap * G, cap * G, B, kLseRows, d.lse_per_seq);
-    const long long full = ((long long)cap * G / kLseRows + B) * H;   // without the empty places
-    const long long chunks = std::min({(1024 + full - 1) / full, (maxL + 511) / 512, 64LL});
-    const long long kc = ((maxL + chunks - 1) / chunks + 63) / 64 * 64;
-    d.lse_kc = (int)std::min(kc, (1LL << 31) - 64);
-    d.lse_chunks = (int)((maxL + d.lse_kc - 1) / d.lse_kc);
-    d.lse_items = tiles * H * d.lse_chunks;
-    d.total = align_up(2 * sizeof(float) * (size_t)cap * p->num_q_heads * d.lse_chunks);
-    return d;
-}
-
-// Keys per chunk of the scores' pass: 1024, down to 256 while there are fewer
-// than 512 workgroups (two per CU).  16 caches of 32K tokens, 8 KV heads: 256
-// keys 254 us, 512 and 1024 220, 2048 229, 4096 258.
-struct StepScorePlan {
-    int kc, chunks, out_chunks, head_copies, head_blocks;
-    long long items, out_items;
-    size_t ml, total;
-};
-StepScorePlan step_score_plan(const logo_problem *p) {
-    StepScorePlan d;
-    const long long maxL = std::max(1, p->max_seqlen), B = p->num_seqs, H = p->num_kv_heads;
-    const long long G = p->num_q_heads / p->num_kv_heads;
-    d.head_copies = G <= 4 ? 4 : G <= 8 ? 2 : 1;
-    d.head_blocks = (int)((G + 15) / 16);
-    d.kc = 1024;
-    while (d.kc > 256 && B * H * d.head_blocks * ((maxL + d.kc - 1) / d.kc) < 512)
-        d.kc /= 2;
-    d.chunks = (int)((maxL + d.kc - 1) / d.kc);
-    d.out_chunks = (int)((maxL + kStepKeys - 1) / kStepKeys);
-    d.items = B * H * d.head_blocks * d.chunks;
-    d.out_items = B * H * d.out_chunks;
-    // (one float behind the scores that nothing reads)
-    d.ml = align_up(sizeof(float) * ((size_t)p->num_q_heads * p->total_tokens + 1));
-    d.total = d.ml + align_up(2 * sizeof(float) * (size_t)B * p->num_q_heads * d.chunks);
-    return d;
-}
-
-struct EvictPlan {
-    long long parts, items;
-    size_t picks, above, total;
-};
-EvictPlan evict_plan(const logo_problem *p) {
-    EvictPlan d;
-    const size_t problems = (size_t)p->num_seqs * p->num_kv_heads;
-    d.parts = std::max(1LL, ((long long)p->max_seqlen + kEvPartRows - 1) / kEvPartRows);
-    d.items = (long long)problems * d.parts;
-    d.picks = d.above = d.total = 0;
-    if (d.parts > 1) {
-        d.picks = align_up(sizeof(uint32_t) * 2 * 1024 * problems * d.parts);
-        d.above = d.picks + align_up(sizeof(uint32_t) * 4 * problems);
-        d.total = d.above + align_up(sizeof(uint32_t) * problems * d.parts);
-    }
-    return d;
 }
 
 int64_t keep_capacity(const logo_problem *p, int32_t budget) {
@@ -1142,8 +1008,8 @@ size_t logo_workspace_bytes(const logo_problem *p, int entry, int32_t sel_capaci
     case LOGO_ENTRY_BWD: return bwd_ws(p, cap).total;
     case LOGO_ENTRY_DENSE_BWD: return dense_bwd_ws(p);
     case LOGO_ENTRY_GLOBAL_BWD: return global_bwd_ws(p, cap).total;
-    case LOGO_ENTRY_CACHE_SCORE: return score_plan(p, cap).total;
-    case LOGO_ENTRY_DECODE_SCORE: return step_score_plan(p).total;
+    case LOGO_ENTRY_CACHE_SCORE: return score_plan(p, cap, SIZE_MAX).total;
+    case LOGO_ENTRY_DECODE_SCORE: return step_score_plan(p, SIZE_MAX).total;
     case LOGO_ENTRY_CACHE_EVICT: return evict_plan(p).total;
     case LOGO_ENTRY_LOCAL:
     case LOGO_ENTRY_COMBINE:
@@ -1782,7 +1648,8 @@ size_t logo_decode_prefix_workspace_bytes(const logo_problem *p, const logo_pref
     if (check_problem(p) != LOGO_OK || check_prefix(p, prefix) != LOGO_OK)
         return 0;
     // (the branches' own tensors make more chunks)
-    return std::max(prefix_plan(p, prefix, false).total, prefix_plan(p, prefix, true).total);
+    return std::max(prefix_plan(p, prefix, false, SIZE_MAX).total,
+                    prefix_plan(p, prefix, true, SIZE_MAX).total);
 }
 
 logo_status logo_decode_prefix(const logo_problem *p, const logo_prefix *prefix,
@@ -1830,7 +1697,7 @@ logo_status logo_decode_prefix(const logo_problem *p, const logo_prefix *prefix,
     a.kp_g = k_pre_g ? k_pre_g : k_pre;
     a.vp_g = v_pre_g ? v_pre_g : v_pre;
     a.share = a.q_g == q && a.k_g == k && a.v_g == v && a.kp_g == k_pre && a.vp_g == v_pre;
-    const PrefixPlan d = prefix_plan(p, prefix, a.share);
+    const PrefixPlan d = prefix_plan(p, prefix, a.share, ws_bytes);
     if (d.first[4] >= (1LL << 31) - 1)
         return LOGO_ERR_UNSUPPORTED;
     if ((st = check_ws(ws, ws_bytes, d.total)) != LOGO_OK)
@@ -1892,7 +1759,7 @@ logo_status logo_cache_score(const logo_problem *p, const logo_bf16 *q, const lo
     const int32_t cap = cu_sel ? sel_capacity : N;
     if ((long long)cap * p->num_q_heads >= (1LL << 31) - 1024)
         return LOGO_ERR_UNSUPPORTED;
-    const ScorePlan d = score_plan(p, cap);
+    const ScorePlan d = score_plan(p, cap, ws_bytes);
     if (d.items >= (1LL << 31) || d.lse_items >= (1LL << 31))
         return LOGO_ERR_UNSUPPORTED;
     if (!lse && cap > 0 && (st = check_ws(ws, ws_bytes, d.total)) != LOGO_OK)
@@ -1949,7 +1816,7 @@ logo_status logo_decode_score(const logo_problem *p, const logo_bf16 *q, const l
                 return LOGO_ERR_SHAPE;
     if (N == 0)
         return LOGO_OK;
-    const StepScorePlan d = step_score_plan(p);
+    const StepScorePlan d = step_score_plan(p, ws_bytes);
     if (d.items >= (1LL << 31) || d.out_items >= (1LL << 31) ||
         (long long)p->num_seqs * p->num_q_heads >= (1LL << 31) ||
         p->num_q_heads / p->num_kv_heads > 8192)

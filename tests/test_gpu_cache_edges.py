@@ -89,3 +89,96 @@ def test_workspace_of_one_stored_byte(pk):
                  lambda: pk.logo_cache_evict(prob, score, 2, k=k, v=k, ws=ws)):
         with pytest.raises(ValueError, match="ws must be contiguous"):
             call()
+
+
+def guarded(nbytes):
+    import torch
+    return torch.full((nbytes + 4096,), 0xA5, dtype=torch.uint8, device="cuda")
+
+
+def close(got, want, tol):
+    e = (got.double() - want.double()).abs()
+    print(f"[edges] max difference {float(e.max()):.3g}", flush=True)
+    assert bool((e <= tol).all())
+
+
+@pytest.mark.parametrize("hq,hkv,d", [(32, 8, 128), (8, 4, 64)])
+@pytest.mark.parametrize("distinct", [False, True], ids=["shared", "own-global"])
+def test_prefix_in_a_longer_step_s_workspace(pk, hq, hkv, d, distinct):
+    """A workspace given for the loop's longest step serves the shorter ones,
+    and nothing is written behind it."""
+    import torch
+    rng = np.random.default_rng(4)
+    P, B = 1500, 4
+    lens = [600, 1, 300, 77]
+    cu = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
+    cup, grp = np.array([0, P], np.int32), np.array([0, B], np.int32)
+    dcu, dcp, dcg = (torch.from_numpy(t).cuda() for t in (cu, cup, grp))
+    N = int(cu[-1])
+    prob = pk.Problem(dcu, hq, hkv, d, 256, cu_seqlens_host=cu)
+    pre = pk.Prefix(dcp, dcg, cu_prefix_host=cup, cu_group_host=grp)
+    q, kp, vp, k, v = (bf16(rng, *s) for s in ((B, hq, d), (P, hkv, d), (P, hkv, d), (N, hkv, d),
+                                               (N, hkv, d)))
+    kw = dict(q_g=bf16(rng, B, hq, d), k_pre_g=vp, v_pre_g=kp, k_g=v, v_g=k) if distinct else {}
+    gate = torch.tensor([0.9, 0.8, 0.1, 0.6], device="cuda")
+    args = (prob, pre, q, kp, vp, k, v, gate)
+    want = pk.logo_decode_prefix(*args, threshold=0.5, **kw)[0]
+    need = pk.logo_decode_prefix_workspace_bytes(prob, pre)
+    # the least: a chunk for each of the four key ranges (two of which the
+    # window may leave empty)
+    least = 4 * B * hq * (d + 2) * 4 + 512
+    for nbytes in (need, need - need // 4, need // 2, least):
+        ws = guarded(nbytes)
+        got = pk.logo_decode_prefix(*args, threshold=0.5, ws=ws[:nbytes], **kw)[0]
+        torch.cuda.synchronize()
+        assert bool((ws[nbytes:] == 0xA5).all()), nbytes
+        # (fp32 sums in another order may round to the next bf16 number)
+        close(got, want, 2.0 ** -7 * want.float().abs() + 1e-5)
+    with pytest.raises(pk.LogoError, match="WORKSPACE"):
+        pk.logo_decode_prefix(*args, threshold=0.5, ws=ws[:256], **kw)
+
+
+def test_score_in_more_rows_workspace(pk):
+    import torch
+    rng = np.random.default_rng(5)
+    N, hq, hkv, d = 9000, 8, 2, 128
+    cu = torch.tensor([0, N], dtype=torch.int32, device="cuda")
+    prob = pk.Problem(cu, hq, hkv, d, 64, cu_seqlens_host=[0, N])
+    q, k = bf16(rng, N, hq, d), bf16(rng, N, hkv, d)
+    sel = torch.arange(N - 40, N, dtype=torch.int32, device="cuda")
+    kw = dict(sel_idx=sel, cu_sel=torch.tensor([0, 40], dtype=torch.int32, device="cuda"))
+    want = pk.logo_cache_score(prob, q, k, **kw)
+    need = pk.logo_workspace_bytes(prob, pk.LOGO_ENTRY_CACHE_SCORE, 40)
+    least = -(-8 * 40 * hq // 256) * 256
+    assert need > 4 * least
+    for nbytes in (need, need // 2, least):
+        ws = guarded(nbytes)
+        got = pk.logo_cache_score(prob, q, k, ws=ws[:nbytes], **kw)
+        torch.cuda.synchronize()
+        assert bool((ws[nbytes:] == 0xA5).all()), nbytes
+        # (the log-sum-exp's terms in other groups: 9000 fp32 additions)
+        close(got, want, want * 9000 * 2.0 ** -24)
+    with pytest.raises(pk.LogoError, match="WORKSPACE"):
+        pk.logo_cache_score(prob, q, k, ws=ws[:least - 256], **kw)
+
+
+def test_step_in_longer_caches_workspace(pk):
+    import torch
+    rng = np.random.default_rng(6)
+    lens, hq, hkv, d = [3000, 1, 2777], 20, 4, 64
+    cu = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
+    prob = pk.Problem(torch.from_numpy(cu).cuda(), hq, hkv, d, 64, cu_seqlens_host=cu)
+    q, k = bf16(rng, 3, hq, d), bf16(rng, int(cu[-1]), hkv, d)
+    gate = torch.tensor([0.9, 0.9, 0.9], device="cuda")
+    want = pk.logo_decode_score(prob, q, k, gate, threshold=0.5)
+    need = pk.logo_workspace_bytes(prob, pk.LOGO_ENTRY_DECODE_SCORE)
+    logits = -(-4 * (hq * int(cu[-1]) + 1) // 256) * 256
+    assert need > logits + 4 * 8 * 3 * hq
+    for nbytes in (need, logits + (need - logits) // 2, logits + 512):
+        ws = guarded(nbytes)
+        got = pk.logo_decode_score(prob, q, k, gate, threshold=0.5, ws=ws[:nbytes])
+        torch.cuda.synchronize()
+        assert bool((ws[nbytes:] == 0xA5).all()), nbytes
+        close(got, want, want * 3000 * 2.0 ** -24)
+    with pytest.raises(pk.LogoError, match="WORKSPACE"):
+        pk.logo_decode_score(prob, q, k, gate, threshold=0.5, ws=ws[:logits])
