@@ -361,7 +361,9 @@ __global__ __launch_bounds__(kScoreThreads, 2) void score_kernel(const ScoreArgs
             lds_gather16(s_row[step % 3][row] + ((lane % kPc) ^ piece_swz<D>(row)) * 8, dst + ld * 1024);
         }
     };
-    float sum[2] = {0.f, 0.f};
+    // (with what its roundings have dropped: a key's sum may have 100 000
+    // blocks of terms)
+    float sum[2] = {0.f, 0.f}, lost[2] = {0.f, 0.f};
     if (steps > 0) {
         meta_put(0, meta_load());
         __syncthreads();
@@ -420,8 +422,12 @@ __global__ __launch_bounds__(kScoreThreads, 2) void score_kernel(const ScoreArgs
                         part[kb] += w;
                     }
             }
-            sum[0] += part[0];
-            sum[1] += part[1];
+#pragma unroll
+            for (int kb = 0; kb < 2; kb++) {
+                const float x = part[kb] - lost[kb], t = sum[kb] + x;
+                lost[kb] = (t - sum[kb]) - x;
+                sum[kb] = t;
+            }
         };
         // rows ascend: the first one's position bounds what all see
         if (uni(pos[0]) < my0 + 63 || (step + 1) * R > rows) {

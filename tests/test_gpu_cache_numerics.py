@@ -132,3 +132,41 @@ def test_prefix_rounds_once(pk, ci, distinct):
         worst = max(worst, float((np.abs(got[b] - want) / tol).max()))
     print(f"[prefix precision case{ci}] worst/tol={worst:.3g}", flush=True)
     assert worst <= 1.0
+
+
+# --- the sums of weights ----------------------------------------------------------
+LONG = [
+    # (tokens, last rows, Hq, Hkv, d): 64, 128 and 256 keys per workgroup
+    (4100, 4100, 8, 1, 64), (9001, 3000, 16, 4, 128), (8200, 4000, 32, 8, 64),
+]
+
+
+@pytest.mark.parametrize("kind", ["one-large", "spread"])
+@pytest.mark.parametrize("ci", range(len(LONG)))
+def test_long_sums_keep_their_small_terms(pk, ci, kind):
+    """Scores of zero and whole log-sum-exps: every weight is a power of two,
+    and a key's sum is off by the roundings of one block of rows (16 terms in a
+    lane), of the sum itself, and of joining two lanes, four waves and what was
+    there before (8) -- not by one for each of its thousands of blocks."""
+    import torch
+    N, n, hq, hkv, d = LONG[ci]
+    rng = np.random.default_rng(5000 + ci)
+    if kind == "one-large":                      # 1 in the first rows, then terms below its steps
+        lse = np.full((hq, n), 24.0, np.float32)
+        lse[:, :40] = 0.0
+    else:
+        lse = rng.integers(0, 20, (hq, n)).astype(np.float32)
+    sel = np.arange(N - n, N).astype(np.int32)
+    dev = to_device(dict(cu=cu_of([N]), sel=sel, cu_sel=cu_of([n]), lse=lse))
+    q = torch.zeros((N, hq, d), dtype=torch.bfloat16, device="cuda")
+    k = torch.ones((N, hkv, d), dtype=torch.bfloat16, device="cuda")
+    prob = pk.Problem(dev["cu"], hq, hkv, d, 64, cu_seqlens_host=cu_of([N]))
+    got = pk.logo_cache_score(prob, q, k, sel_idx=dev["sel"], cu_sel=dev["cu_sel"], lse=dev["lse"])
+    got = got.cpu().numpy().astype(np.float64)
+    w = np.exp2(-lse.astype(np.float64)).reshape(hkv, hq // hkv, n).sum(1)
+    later = np.cumsum(w[:, ::-1], axis=1)[:, ::-1]             # rows at or after each
+    want = np.concatenate([np.repeat(later[:, :1], N - n, 1), later], 1)
+    tol = (16 + 2 + 8) * 2.0 ** -24 * want
+    worst = float((np.abs(got - want) / tol).max())
+    print(f"[score sums {kind} case{ci}] worst/tol={worst:.3g}", flush=True)
+    assert worst <= 1.0
