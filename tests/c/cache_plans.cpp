@@ -33,6 +33,14 @@ void step_plan(const logo_problem *p, size_t room, long long out[3]) {
     out[2] = d.chunks;
 }
 
+int score_key_waves(const logo_problem *p, int cap) {
+    return logo::score_plan(p, cap, SIZE_MAX).key_waves;
+}
+
+int step_head_copies(const logo_problem *p) {
+    return logo::step_score_plan(p, SIZE_MAX).head_copies;
+}
+
 long long evict_total(const logo_problem *p) { return (long long)logo::evict_plan(p).total; }
 
 }  // extern "C"

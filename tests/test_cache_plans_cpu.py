@@ -193,3 +193,23 @@ def test_evict_workspace_grows(plans, lib):
         need = lib.logo_workspace_bytes(ctypes.byref(p), pk.LOGO_ENTRY_CACHE_EVICT, 0)
         assert need == plans.evict_total(ctypes.byref(p)) >= last
         last = need
+
+
+def test_shapes_reach_their_paths(plans):
+    """The shapes that the GPU tests run take the kernels' larger variants."""
+    import _cache_shapes as shapes
+    seen = set()
+    for (lens, rows, hq, hkv, d), waves in shapes.SCORES:
+        p = problem(len(lens), sum(lens), max(lens), hq, hkv, d, 64)
+        assert plans.score_key_waves(ctypes.byref(p), sum(rows)) == waves
+        seen.add((waves, d))
+    assert seen == {(w, d) for w in (2, 4) for d in (64, 128)}
+    seen = set()
+    for (lens, hq, hkv, d), kc in shapes.STEPS:
+        p = problem(len(lens), sum(lens), max(lens), hq, hkv, d, 64)
+        assert small(plans, "step_plan", p, ALL)["kc"] == kc
+        seen.add((kc, d, plans.step_head_copies(ctypes.byref(p))))
+        # a wave's half of a chunk, 16 keys a slot, against the ring's slots
+        if kc == 1024:
+            assert kc // 2 // 16 >= 2 * {64: 16, 128: 8}[d]
+    assert seen >= {(kc, d, c) for kc in (512, 1024) for d in (64, 128) for c in (1, 2, 4)}
