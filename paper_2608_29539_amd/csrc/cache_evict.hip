@@ -419,10 +419,10 @@ hipError_t launch_cache_evict(const EvictArgs &a, hipStream_t s) {
         hipLaunchKernelGGL(evict_rank_kernel, grid_s, block, 0, s, a);
         e = hipGetLastError();
     }
-    if (e != hipSuccess || (!a.in[0] && !a.in[2]) || a.cap == 0)
+    if (e != hipSuccess || (!a.in[0] && !a.in[2]) || a.rows == 0)
         return e;
-    const int rows = 256 / (a.head_dim / 8);               // per workgroup
-    const dim3 grid(((int64_t)a.cap * a.hkv + rows - 1) / rows);
+    const int per = 256 / (a.head_dim / 8);                // rows per workgroup
+    const dim3 grid(((int64_t)a.rows * a.hkv + per - 1) / per);
     if (a.head_dim == 128)
         hipLaunchKernelGGL((evict_copy_kernel<128>), grid, dim3(256), 0, s, a);
     else

@@ -77,6 +77,7 @@ struct EvictArgs {
     const int32_t *cu;
     int64_t n;
     int32_t num_seqs, hkv, head_dim, budget, recent, cap;
+    int32_t rows;                            // of the outputs, at most (cap may be larger)
     const uint16_t *in[4];
     uint16_t *out[4];
     float *score_out;                        // [Hkv][cap]

@@ -1884,11 +1884,12 @@ logo_status logo_cache_evict(const logo_problem *p, const float *score, int32_t 
     }
     if (p->total_tokens > 0 && (!score || !score_out || !keep_idx))
         return LOGO_ERR_NULL;
-    if (capacity < keep_capacity(p, budget))
+    const int64_t rows = keep_capacity(p, budget);
+    if (capacity < rows)
         return LOGO_ERR_SHAPE;
     const EvictPlan d = evict_plan(p);
     if (d.items >= (1LL << 31) || (long long)p->num_seqs * p->num_kv_heads >= (1LL << 29) ||
-        (long long)capacity * p->num_kv_heads * (p->head_dim / 8) / 256 >= (1LL << 31) - 1)
+        rows * p->num_kv_heads * (p->head_dim / 8) / 256 >= (1LL << 31) - 1)
         return LOGO_ERR_UNSUPPORTED;
     if ((st = check_ws(ws, ws_bytes, d.total)) != LOGO_OK)
         return st;
@@ -1903,6 +1904,7 @@ logo_status logo_cache_evict(const logo_problem *p, const float *score, int32_t 
     a.budget = budget;
     a.recent = recent;
     a.cap = capacity;
+    a.rows = (int32_t)rows;
     for (int i = 0; i < 4; i++) {
         a.in[i] = in[i];
         a.out[i] = out[i];

@@ -182,3 +182,27 @@ def test_step_in_longer_caches_workspace(pk):
         close(got, want, want * 3000 * 2.0 ** -24)
     with pytest.raises(pk.LogoError, match="WORKSPACE"):
         pk.logo_decode_score(prob, q, k, gate, threshold=0.5, ws=ws[:logits])
+
+
+def test_evict_into_far_more_room_than_rows(pk):
+    """A capacity far above the kept rows (the stride of score_out and
+    keep_idx; one head has no second row of them)."""
+    import ctypes
+
+    import torch
+    L, cap = 300, 1 << 30
+    cu = torch.tensor([0, L], dtype=torch.int32, device="cuda")
+    prob = pk.Problem(cu, 1, 1, 64, 8, cu_seqlens_host=[0, L])
+    rng = np.random.default_rng(7)
+    k, v, score = bf16(rng, L, 1, 64), bf16(rng, L, 1, 64), torch.rand((1, L), device="cuda")
+    want = pk.logo_cache_evict(prob, score, 40, recent=5, k=k, v=v)
+    got = {n: torch.zeros_like(t) for n, t in want.items() if t is not None}
+    p = {n: ctypes.c_void_p(t.data_ptr()) for n, t in dict(got, k=k, v=v, score=score).items()}
+    st = pk.library().logo_cache_evict(
+        prob.c, p["score"], 40, 5, p["k"], p["v"], None, None, p["k_out"], p["v_out"], None, None,
+        p["score_out"], p["keep_idx"], p["cu_keep"], cap, None, 0,
+        ctypes.c_void_p(torch.cuda.current_stream().cuda_stream))
+    torch.cuda.synchronize()
+    assert st == 0, pk.logo_status_str(st)
+    for n in got:
+        assert torch.equal(got[n], want[n]), n
