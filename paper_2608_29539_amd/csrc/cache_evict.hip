@@ -30,7 +30,6 @@
 namespace logo {
 namespace {
 
-constexpr int kEvThreads = 1024;                           // of a part of kEvPartRows
 constexpr int kEvPer = kEvPartRows / kEvThreads;           // rows per thread
 constexpr int kEvBins = 2048;
 
@@ -400,8 +399,8 @@ hipError_t launch_cache_evict(const EvictArgs &a, hipStream_t s) {
     const dim3 grid_s(a.num_seqs * a.hkv * a.parts), block(kEvThreads);
     hipError_t e;
     if (a.small) {
-        hipLaunchKernelGGL((evict_select_kernel<kEvSmallRows / kEvPer>), grid_s,
-                           dim3(kEvSmallRows / kEvPer), 0, s, a);
+        hipLaunchKernelGGL((evict_select_kernel<kEvSmallThreads>), grid_s, dim3(kEvSmallThreads),
+                           0, s, a);
         e = hipGetLastError();
     } else if (a.parts == 1) {
         hipLaunchKernelGGL((evict_select_kernel<kEvThreads>), grid_s, block, 0, s, a);

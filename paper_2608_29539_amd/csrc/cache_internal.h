@@ -38,6 +38,7 @@ struct PrefixArgs {
 hipError_t launch_decode_prefix(const PrefixArgs &a, hipStream_t s);
 
 // Attention weight received by every key (cache_score.hip).
+constexpr int kScoreThreads = 256;
 struct ScoreArgs {
     const uint16_t *q, *k;
     const int32_t *cu, *sel_idx, *cu_sel;    // cu_sel NULL: every token is a row
@@ -54,6 +55,7 @@ struct ScoreArgs {
 };
 hipError_t launch_cache_score(const ScoreArgs &a, hipStream_t s);
 
+constexpr int kStepThreads = 128;           // of the scores' pass; the weights' kScoreThreads
 struct StepScoreArgs {
     const uint16_t *q, *k;
     const int32_t *cu;
@@ -89,7 +91,9 @@ struct EvictArgs {
     int32_t small;                           // no cache of more than kEvSmallRows
     uint32_t *hist, *picks, *above;
 };
+constexpr int kEvThreads = 1024;            // of a part of kEvPartRows
 constexpr int kEvSmallRows = 2048;
+constexpr int kEvSmallThreads = kEvSmallRows / (kEvPartRows / kEvThreads);
 hipError_t launch_cache_evict(const EvictArgs &a, hipStream_t s);
 
 }  // namespace logo

@@ -26,7 +26,6 @@
 namespace logo {
 namespace {
 
-constexpr int kScoreThreads = 256;
 constexpr int kScoreWaves = kScoreThreads / 64;
 constexpr int kLseBuffers = 4;
 
@@ -490,7 +489,7 @@ __global__ __launch_bounds__(kScoreThreads, 2) void score_kernel(const ScoreArgs
 // caches of 32K tokens, 8 KV heads: 1.14 GB in 220 us, 5.2 TB/s (278 us with
 // fragments loaded from global memory).
 // ---------------------------------------------------------------------------
-constexpr int kStepWaves = 2;
+constexpr int kStepWaves = kStepThreads / 64;
 template <int D>
 constexpr int step_ring() { return D == 128 ? 8 : 16; }
 
@@ -502,7 +501,7 @@ __device__ __forceinline__ void wait_outstanding() {
 }
 
 template <int D, int P>
-__global__ __launch_bounds__(kStepWaves * 64) void step_logits_kernel(const StepScoreArgs a) {
+__global__ __launch_bounds__(kStepThreads) void step_logits_kernel(const StepScoreArgs a) {
     constexpr int kRing = step_ring<D>(), kPc = D / 8;
     constexpr int kLoads = 16 * D * 2 / 1024;              // loads per slot
     constexpr int kCopies = 4 / P;
@@ -741,7 +740,7 @@ hipError_t launch_cache_score(const ScoreArgs &a, hipStream_t s) {
 hipError_t launch_decode_score(const StepScoreArgs &a, hipStream_t s) {
     auto launch = [&](auto d, auto p) {
         hipLaunchKernelGGL((step_logits_kernel<decltype(d)::value, decltype(p)::value>),
-                           dim3(a.items), dim3(kStepWaves * 64), 0, s, a);
+                           dim3(a.items), dim3(kStepThreads), 0, s, a);
     };
     auto launch_d = [&](auto d) {
         if (a.head_copies == 4)

@@ -391,6 +391,10 @@ int64_t keep_capacity(const logo_problem *p, int32_t budget) {
     return s;
 }
 
+// A launch of `groups` workgroups of `threads` threads is too large: HIP takes
+// fewer than 2^32 threads.
+bool too_many(long long groups, int threads) { return groups >= (1LL << 32) / threads; }
+
 bool misaligned(const void *p) { return ((uintptr_t)p % 16) != 0; }
 
 // The threshold of a decoding step (host value or device scalar).
@@ -1698,7 +1702,8 @@ logo_status logo_decode_prefix(const logo_problem *p, const logo_prefix *prefix,
     a.vp_g = v_pre_g ? v_pre_g : v_pre;
     a.share = a.q_g == q && a.k_g == k && a.v_g == v && a.kp_g == k_pre && a.vp_g == v_pre;
     const PrefixPlan d = prefix_plan(p, prefix, a.share, ws_bytes);
-    if (d.first[4] >= (1LL << 31) - 1)
+    if (too_many(d.first[4] + 1, kPrefixThreads) ||
+        too_many(((long long)p->num_seqs * p->num_q_heads + 3) / 4, 256))
         return LOGO_ERR_UNSUPPORTED;
     if ((st = check_ws(ws, ws_bytes, d.total)) != LOGO_OK)
         return st;
@@ -1760,7 +1765,7 @@ logo_status logo_cache_score(const logo_problem *p, const logo_bf16 *q, const lo
     if ((long long)cap * p->num_q_heads >= (1LL << 31) - 1024)
         return LOGO_ERR_UNSUPPORTED;
     const ScorePlan d = score_plan(p, cap, ws_bytes);
-    if (d.items >= (1LL << 31) || d.lse_items >= (1LL << 31))
+    if (too_many(d.items, kScoreThreads) || too_many(lse ? 0 : d.lse_items, kScoreThreads))
         return LOGO_ERR_UNSUPPORTED;
     if (!lse && cap > 0 && (st = check_ws(ws, ws_bytes, d.total)) != LOGO_OK)
         return st;
@@ -1817,7 +1822,7 @@ logo_status logo_decode_score(const logo_problem *p, const logo_bf16 *q, const l
     if (N == 0)
         return LOGO_OK;
     const StepScorePlan d = step_score_plan(p, ws_bytes);
-    if (d.items >= (1LL << 31) || d.out_items >= (1LL << 31) ||
+    if (too_many(d.items, kStepThreads) || too_many(d.out_items, kScoreThreads) ||
         (long long)p->num_seqs * p->num_q_heads >= (1LL << 31) ||
         p->num_q_heads / p->num_kv_heads > 8192)
         return LOGO_ERR_UNSUPPORTED;
@@ -1888,8 +1893,9 @@ logo_status logo_cache_evict(const logo_problem *p, const float *score, int32_t 
     if (capacity < rows)
         return LOGO_ERR_SHAPE;
     const EvictPlan d = evict_plan(p);
-    if (d.items >= (1LL << 31) || (long long)p->num_seqs * p->num_kv_heads >= (1LL << 29) ||
-        rows * p->num_kv_heads * (p->head_dim / 8) / 256 >= (1LL << 31) - 1)
+    const bool is_small = p->max_seqlen <= kEvSmallRows;
+    if (too_many(d.items, is_small ? kEvSmallThreads : kEvThreads) ||
+        ((k || k_g) && too_many((rows * p->num_kv_heads * (p->head_dim / 8) + 255) / 256, 256)))
         return LOGO_ERR_UNSUPPORTED;
     if ((st = check_ws(ws, ws_bytes, d.total)) != LOGO_OK)
         return st;
@@ -1913,7 +1919,7 @@ logo_status logo_cache_evict(const logo_problem *p, const float *score, int32_t 
     a.keep_idx = keep_idx;
     a.cu_keep = cu_keep;
     a.parts = (int32_t)d.parts;
-    a.small = p->max_seqlen <= kEvSmallRows;
+    a.small = is_small;
     a.hist = (uint32_t *)ws;
     a.picks = (uint32_t *)((char *)ws + d.picks);
     a.above = (uint32_t *)((char *)ws + d.above);
