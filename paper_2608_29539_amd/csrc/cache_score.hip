@@ -520,7 +520,7 @@ __global__ __launch_bounds__(kStepThreads) void step_logits_kernel(const StepSco
         return;
     const int base = a.cu[b];
     const int L = a.cu[b + 1] - base;
-    const int k0 = c * a.kc, k1 = min(L, k0 + a.kc);
+    const int k0 = c * a.kc, k1 = k0 + min(L - k0, a.kc);   // (a chunk may be 2^30 keys)
     if (k0 >= k1)
         return;
     // this wave's keys: its share of the chunk's blocks of 64

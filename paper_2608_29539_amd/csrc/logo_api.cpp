@@ -395,6 +395,13 @@ int64_t keep_capacity(const logo_problem *p, int32_t budget) {
 // fewer than 2^32 threads.
 bool too_many(long long groups, int threads) { return groups >= (1LL << 32) / threads; }
 
+// Positions of N rows and the ends of the blocks behind them, and the byte
+// offsets inside a tile of `rows` rows, are 32-bit.
+bool past_32_bits(const logo_problem *p, int rows) {
+    return p->total_tokens > INT32_MAX - 2048 ||
+           (long long)p->num_kv_heads * p->head_dim * 2 * rows >= (1LL << 31);
+}
+
 bool misaligned(const void *p) { return ((uintptr_t)p % 16) != 0; }
 
 // The threshold of a decoding step (host value or device scalar).
@@ -1762,7 +1769,8 @@ logo_status logo_cache_score(const logo_problem *p, const logo_bf16 *q, const lo
     if (N == 0)
         return LOGO_OK;
     const int32_t cap = cu_sel ? sel_capacity : N;
-    if ((long long)cap * p->num_q_heads >= (1LL << 31) - 1024)
+    if ((long long)cap * p->num_q_heads >= (1LL << 31) - 1024 ||
+        past_32_bits(p, lse ? 1 : kBlockN))
         return LOGO_ERR_UNSUPPORTED;
     const ScorePlan d = score_plan(p, cap, ws_bytes);
     if (too_many(d.items, kScoreThreads) || too_many(lse ? 0 : d.lse_items, kScoreThreads))
@@ -1824,7 +1832,7 @@ logo_status logo_decode_score(const logo_problem *p, const logo_bf16 *q, const l
     const StepScorePlan d = step_score_plan(p, ws_bytes);
     if (too_many(d.items, kStepThreads) || too_many(d.out_items, kScoreThreads) ||
         (long long)p->num_seqs * p->num_q_heads >= (1LL << 31) ||
-        p->num_q_heads / p->num_kv_heads > 8192)
+        p->num_q_heads / p->num_kv_heads > 8192 || past_32_bits(p, 16))
         return LOGO_ERR_UNSUPPORTED;
     if ((st = check_ws(ws, ws_bytes, d.total)) != LOGO_OK)
         return st;

@@ -67,3 +67,17 @@ def test_launches_of_2_to_the_32_threads(lib):
     assert evict(lib, problem(1 << 18, 1 << 21, 1 << 14, 8, 8), 1 << 21) == ERR_UNSUPPORTED
     assert evict(lib, problem(1 << 21, 1 << 21, 1, 8, 8), 1 << 21) == ERR_UNSUPPORTED
     assert evict(lib, problem(2, 1 << 25, 1 << 24, 8, 8), 1 << 25) == ERR_UNSUPPORTED
+
+
+def test_rows_next_to_2_to_the_31(lib):
+    """The end of a block of keys behind the last row passes 2^31."""
+    for n in ((1 << 31) - 100, (1 << 31) - 1):
+        assert score(lib, problem(1, n, n, 1, 1, 64), 8, True) == ERR_UNSUPPORTED
+        assert score(lib, problem(1, n, n, 1, 1, 64), 8, False) == ERR_UNSUPPORTED
+        assert step(lib, problem(1, n, n, 1, 1, 64)) == ERR_UNSUPPORTED
+
+
+def test_tiles_of_2_gib(lib):
+    """A tile's rows of so many heads that its byte offsets pass 2^31."""
+    assert score(lib, problem(1, 100, 100, 1 << 17, 1 << 17), 8, False) == ERR_UNSUPPORTED
+    assert step(lib, problem(1, 100, 100, 1 << 19, 1 << 19)) == ERR_UNSUPPORTED
