@@ -828,10 +828,9 @@ def _checks_here(prob: Problem):
         for t in tensors:
             if t is not None and t.get_device() != dev:
                 raise ValueError(f"tensor on {t.device}, but the current device is {dev}")
-        if ws is not None:
-            here(ws)
-            if not ws.is_contiguous():           # (its numel() bytes lie behind each other)
-                raise ValueError("ws must be contiguous")
+        if ws is not None and (ws.get_device() != dev or not ws.is_contiguous()):
+            # (its numel() bytes lie behind each other)
+            raise ValueError(f"ws must be contiguous, on device {dev}")
 
     def check(t, dtype, shape, name):
         if (t is not None and t.dtype == dtype and t.get_device() == dev and t.is_contiguous()

@@ -51,8 +51,9 @@ struct PrefixPlan {
 // Keys per chunk.  The prefix's part of the global branch: about 320
 // workgroups over the KV heads and row tiles (one per CU and some, the other
 // ranges' beside them), at least 256 keys each: 32 sequences behind 16K tokens
-// 45.9 us (512 workgroups 49.9), 64 behind 32K 76.3 (256: 79.0, 512: 80.7, 128:
-// 122), three groups behind 17.6K in all 21.9 (384 of at least 128 keys: 25.6).
+// 45.9 us (with 256, 384 and 512 workgroups 46.6, 47.2, 51.3), 64 behind 32K 88.7
+// (87.1, 85.1, 86.6), three groups behind 17.6K in all 23.0 (23.9, 23.1, 23.2; 384
+// of at least 128 keys 25.6 where 256 were 21.9).
 // The sequences' own rows: 512 keys, 256 where that makes fewer than 512
 // workgroups (23 sequences, 2 KV heads: 32 and 24 us; 32 and 8: 38 and 39).
 // The window's part of a prefix: 256.  At most kMaxPrefixChunks each; fewer
