@@ -12,8 +12,9 @@
 //   evict_select_kernel  caches of up to 8192 rows: one workgroup per (sequence,
 //                        KV head) does it all, with the histograms in LDS (up
 //                        to 2048 rows of 256 threads, whose barriers and scans
-//                        are shorter: 4 caches of 2048 rows 7.5 us, 10.1 with
-//                        1024)
+//                        are shorter: 4 caches of 2048 rows 7.4 us, 10.1 with
+//                        1024; a call that is waited for 27.8 and 30.5 us, one
+//                        among others 13.1-13.5 with both: its enqueuing)
 //   evict_hist_kernel    longer ones: a launch per digit, in which every part
 //                        of 8192 rows adds up all parts' last histograms, picks
 //                        the bin of the k-th and counts the next digit

@@ -217,10 +217,11 @@ __global__ __launch_bounds__(kScoreThreads, 2) void score_lse_kernel(const Score
 // for no chain of loads.  A row's 16-byte pieces are permuted (piece_swz).
 // Each Q fragment feeds two products (the wave's two blocks of 32 keys), and
 // the exponentials of one block of rows are issued between the products of the
-// next.  4096 rows on 32768 keys, 32 / 8 heads: 590 us, 930
-// TFLOP/s (1088 with rows staged through registers in 64-row steps); matrix
-// cores busy in 44% of the cycles, the vector unit in 58%, of which the
-// exponentials are half.
+// next.  A key's sum is compensated: what an addition drops is taken off the
+// next block's sum.  4096 rows on 32768 keys, 32 / 8 heads: 576-606 us on four
+// cards, 910-955 TFLOP/s, with or without that (1088 with rows staged through
+// registers in 64-row steps); matrix cores busy in 44% of the cycles, the vector
+// unit in 59%, of which the exponentials are half.
 // ---------------------------------------------------------------------------
 constexpr int kScoreRows = 128;
 

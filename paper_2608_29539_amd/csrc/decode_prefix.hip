@@ -31,11 +31,12 @@
 // is fp32.
 //
 // Bounds (32 / 8 heads, d = 128).  32 sequences behind 16K tokens, 4 selected:
-// reading 171 MB, 31 us + 5.9 of merge (5.5 TB/s from the last-level cache).
+// reading 171 MB, 31 us + 5.6 of merge (5.5 TB/s from the last-level cache).
 // 64 behind 32K, all selected: a wave's chain per tile (fragment reads, the
-// running max, exponentials, two products of 256 cycles), 69 us + 7.6 for 36
-// GFLOP; 64-key tiles and deeper or shallower prefetch took the same time.
-// Small steps: the prologue (4 us of dependent loads) and the merge's.
+// running max, exponentials, products of 256 and 512 cycles), 87 us + 7.5 for 36
+// GFLOP (54 with both parts of P); 64-key tiles and deeper or shallower prefetch
+// took the same time.  Small steps: the prologue (4 us of dependent loads) and the
+// merge's.
 #include "cache_internal.h"
 #include "cache_tiles.h"
 #include "decode_common.h"
